@@ -478,3 +478,10 @@ def lossy_step_fused_noalloc(*, d: int, packet: int, step: int, loss_g: LossSpec
     head, tail = _fused_args(d, packet, step, loss_g, loss_b, grads, opt, theta, replicas, m, v,
                              ge_state_g, ge_state_b, arrived_g, arrived_b, counts, drift, ext)
     _check("lossy_step_fused_noalloc", _load().lossy_step_fused_noalloc(*head, *tail))
+
+
+# The workers' side of the step; it builds on the helpers above.
+from . import local as _local  # noqa: E402
+from .local import *  # noqa: E402,F401,F403
+
+__all__ += _local.__all__

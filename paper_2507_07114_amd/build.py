@@ -31,7 +31,7 @@ COMMON = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     f"-I{INCLUDE}", f"-I{CSRC}",
 ]
-SOURCES = ["kernels.hip", "api.cpp"]
+SOURCES = ["kernels.hip", "api.cpp", "local.hip", "local_api.cpp"]
 PROBE_SOURCES = ["probe.hip"]
 
 

@@ -9,6 +9,7 @@
 #include <cstdio>
 #include <string>
 
+#include "errors.h"
 #include "kernels.h"
 
 using namespace lossy;
@@ -22,8 +23,10 @@ static_assert(LL_PACE_AUTO == kPaceAuto && LL_PACE_ALWAYS == kPaceAlways &&
               "pacing modes");
 
 namespace {
-
 thread_local std::string g_error;
+}
+
+namespace lossy {
 
 int fail(int code, const char* fmt, ...) {
     char buf[512];
@@ -45,7 +48,36 @@ int hip_check(hipError_t e, const char* what) {
     return ok();
 }
 
+size_t elem_bytes(int32_t dtype) { return dtype == LL_BF16 ? 2 : 4; }
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Rows [n][ld] of elements of `esize` bytes: every row starts on a 16-byte
+// boundary when the base does and ld * esize is a multiple of 16.
+int check_rows(const char* name, const void* p, int64_t ld, int64_t d, size_t esize) {
+    if (!p) return fail(LL_EINVAL, "%s is NULL", name);
+    if (ld < d) return fail(LL_EINVAL, "%s: ld=%lld < d=%lld", name, (long long)ld, (long long)d);
+    if (((size_t)ld * esize) % 16 != 0)
+        return fail(LL_EALIGN, "%s: ld=%lld elements of %zu bytes is not a multiple of 16 bytes",
+                    name, (long long)ld, esize);
+    if (!aligned16(p)) return fail(LL_EALIGN, "%s is not 16-byte aligned", name);
+    return LL_OK;
+}
+
+int check_vec(const char* name, const void* p, bool required) {
+    if (!p) return required ? fail(LL_EINVAL, "%s is NULL", name) : LL_OK;
+    if (!aligned16(p)) return fail(LL_EALIGN, "%s is not 16-byte aligned", name);
+    return LL_OK;
+}
+
+int check_dtype(const char* name, int32_t t) {
+    if (t != LL_F32 && t != LL_BF16) return fail(LL_EINVAL, "%s: unknown dtype %d", name, t);
+    return LL_OK;
+}
+
+}  // namespace lossy
+
+namespace {
 
 // ceil(p * 2^32): hi32(w) < thr  <=>  hi32(w) / 2^32 < p.
 uint64_t threshold(double p) { return (uint64_t)std::ceil(p * 4294967296.0); }
@@ -70,31 +102,6 @@ int check_shape(int32_t n, int64_t d, int64_t packet, Geometry* g) {
     g->blocks = g->P * ((packet + chunk - 1) / chunk);
     if (g->blocks > 0x7FFFFFFFll)
         return fail(LL_EINVAL, "too many workgroups (%lld)", (long long)g->blocks);
-    return LL_OK;
-}
-
-size_t elem_bytes(int32_t dtype) { return dtype == LL_BF16 ? 2 : 4; }
-
-// Rows [n][ld] of elements of `esize` bytes: every row starts on a 16-byte
-// boundary when the base does and ld * esize is a multiple of 16.
-int check_rows(const char* name, const void* p, int64_t ld, int64_t d, size_t esize) {
-    if (!p) return fail(LL_EINVAL, "%s is NULL", name);
-    if (ld < d) return fail(LL_EINVAL, "%s: ld=%lld < d=%lld", name, (long long)ld, (long long)d);
-    if (((size_t)ld * esize) % 16 != 0)
-        return fail(LL_EALIGN, "%s: ld=%lld elements of %zu bytes is not a multiple of 16 bytes",
-                    name, (long long)ld, esize);
-    if (!aligned16(p)) return fail(LL_EALIGN, "%s is not 16-byte aligned", name);
-    return LL_OK;
-}
-
-int check_vec(const char* name, const void* p, bool required) {
-    if (!p) return required ? fail(LL_EINVAL, "%s is NULL", name) : LL_OK;
-    if (!aligned16(p)) return fail(LL_EALIGN, "%s is not 16-byte aligned", name);
-    return LL_OK;
-}
-
-int check_dtype(const char* name, int32_t t) {
-    if (t != LL_F32 && t != LL_BF16) return fail(LL_EINVAL, "%s: unknown dtype %d", name, t);
     return LL_OK;
 }
 
