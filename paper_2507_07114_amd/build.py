@@ -31,7 +31,8 @@ COMMON = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     f"-I{INCLUDE}", f"-I{CSRC}",
 ]
-SOURCES = ["kernels.hip", "api.cpp", "local.hip", "local_api.cpp"]
+SOURCES = ["kernels.hip", "api.cpp", "local_embed.hip", "local_act.hip", "local_wgrad.hip",
+           "local_api.cpp"]
 PROBE_SOURCES = ["probe.hip"]
 
 
