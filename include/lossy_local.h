@@ -130,7 +130,7 @@ LL_API int ll_act_unpack(int32_t n, int64_t t, int64_t h, const int32_t* lengths
  * as a sum of three bf16 terms that hold all its bits, but for what lies
  * below 2^-126), sums are fp32.
  *   dy         [n][t][ld_y] of ydtype, ld_y >= o.
- *   q, s       as ll_act_pack writes them.
+ *   q, s       as ll_act_pack writes them.  ld_y, ld_q and ld_s are below 2^24.
  *   workspace  ws_bytes >= ll_act_wgrad_workspace_bytes(n, t, o, h); may be
  *              NULL where that is 0.
  */

@@ -211,6 +211,11 @@ int ll_act_wgrad(int32_t n, int64_t t, int64_t o, int64_t h, const int32_t* leng
     if (t > 0) {
         if ((r = check_act("dy", dy, ld_y, o, elem_bytes(ydtype)))) return r;
         if ((r = check_pack(q, ld_q, s, ld_s, h))) return r;
+        // the kernel addresses 32 rows with 31-bit byte offsets
+        const int64_t most = 1 << 24;
+        if (ld_y >= most || ld_q >= most || ld_s >= most)
+            return fail(LL_EINVAL, "dy, q, s: ld=%lld, %lld, %lld not below 2^24", (long long)ld_y,
+                        (long long)ld_q, (long long)ld_s);
     }
     if ((r = check_workspace(workspace, ws_bytes, act_wgrad_workspace(n, t, o, h)))) return r;
     WgradParams p;

@@ -41,6 +41,9 @@ constexpr int unit_of() {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// Descriptor word of a raw buffer (offsets in bytes, no format, no swizzle).
+constexpr int kBufferRaw = 0x00020000;
+
 // Raw memory accesses of 4, 8 or 16 bytes at any element's alignment: global
 // memory takes such vectors at any address, so rows that start anywhere need no
 // element-by-element form.  STREAM: non-temporal, for data that the call touches once.

@@ -1,5 +1,12 @@
 // Weight gradient of a linear layer from an 8-bit checkpoint of its input
 // (include/lossy_local.h): ll_act_wgrad.
+//
+// D[o][h] = sum_t dy[t][o] x^[t][h] on the bf16 matrix units.  x^ = code * 2^k
+// is exact in bf16 (4 significant bits), so bf16 dy needs one product per
+// element; fp32 dy is a sum of three bf16 terms, taken as three times as many
+// tokens.  Both factors lie token by token, the matrix units want each lane's
+// tokens side by side: LDS holds the tiles as they come and the transposing
+// LDS read turns them.
 #include <hip/hip_runtime.h>
 
 #include "local.h"
@@ -9,62 +16,413 @@ namespace lossy {
 
 namespace {
 
-__device__ __forceinline__ float e4m3_value(uint32_t code, uint32_t s) {
-    return __builtin_amdgcn_cvt_f32_fp8((int)code, 0) * __uint_as_float(s << 23);
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) i16x4 LdsQuad;
+
+constexpr int kStepT = 32;    // tokens of a step
+constexpr int kStages = 3;    // steps whose tiles are in LDS
+constexpr int kWgThreads = 256;
+
+struct WgradPlan {
+    int64_t tiles_o, tiles_h;
+    int splits;         // runs of tokens summed apart
+    int64_t split_t;    // tokens of a run, a multiple of kStepT
+    float* part;        // [splits][n][o][h] where splits > 1
+};
+
+// A tile row (one token, T columns of bf16) is T / 16 units of 32 bytes; unit u
+// of row k lies at u ^ 2 (k % 4).  The transposing read of 16 lanes takes 32
+// bytes from 4 consecutive rows; with the exchange these and the neighbouring
+// 16 lanes' fall on different banks.
+__device__ __forceinline__ int unit_at(int k, int unit) { return unit ^ (2 * (k & 3)); }
+
+// The bf16 terms of an fp32 value: the leading 8 significant bits, the next 8
+// and the rest, each cut off (so that every difference is exact).  What is
+// not finite has one term.
+__device__ __forceinline__ uint32_t f32_term(float x, int part) {
+    const uint32_t u = __float_as_uint(x);
+    const uint32_t hi = u & 0xFFFF0000u;
+    if ((u & 0x7F800000u) == 0x7F800000u)
+        return part ? 0u : (u & 0x7FFFFFu ? 0x7FC0u : hi >> 16);
+    if (part == 0) return hi >> 16;
+    const float r = x - __uint_as_float(hi);
+    const uint32_t mid = __float_as_uint(r) & 0xFFFF0000u;
+    if (part == 1) return mid >> 16;
+    return __float_as_uint(r - __uint_as_float(mid)) >> 16;
 }
 
-// ---- weight gradient ----------------------------------------------------------
+// 8 columns of dy of one token, and one column.
+template <class Y>
+struct Chunk8;
+template <>
+struct Chunk8<El16> {
+    u32x4 a;
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+        a = __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
+    }
+    __device__ __forceinline__ u32x4 terms(int) const { return a; }
+    static __device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+        return __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t term1(uint32_t x, int) { return x; }
+};
+template <>
+struct Chunk8<El32> {
+    u32x4 a, b;
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+        a = __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
+        b = __builtin_amdgcn_raw_buffer_load_b128(r, at + 16, 0, 0);
+    }
+    __device__ __forceinline__ u32x4 terms(int part) const {
+        auto two = [&](uint32_t lo, uint32_t hi) {
+            return f32_term(__uint_as_float(lo), part) | f32_term(__uint_as_float(hi), part) << 16;
+        };
+        return u32x4{two(a.x, a.y), two(a.z, a.w), two(b.x, b.y), two(b.z, b.w)};
+    }
+    static __device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+        return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t term1(uint32_t x, int part) {
+        return f32_term(__uint_as_float(x), part);
+    }
+};
 
-constexpr int kWT = 32;  // tile edge and tokens a turn
+// bf16 values of 8 codes under one scale.
+__device__ __forceinline__ u32x4 restore8(u32x2 code, uint32_t s) {
+    const float scale = __uint_as_float(s << 23);
+    auto two = [&](uint32_t w, bool hi) {
+        const bf16x2 v = hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, scale, true)
+                            : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, scale, false);
+        uint32_t r;
+        __builtin_memcpy(&r, &v, 4);
+        return r;
+    };
+    return u32x4{two(code.x, false), two(code.x, true), two(code.y, false), two(code.y, true)};
+}
 
-template <class Y, class G>
-__global__ __launch_bounds__(kBlock) void k_act_wgrad(WgradParams p) {
+// Staging registers of one step of one thread: 8 columns of kPass token rows,
+// and an element of the columns past the last whole 8.
+template <class Y, int TO, int TH>
+struct Staged {
+    static constexpr int kPassY = kStepT * TO / 8 / kWgThreads;
+    static constexpr int kPassX = kStepT * TH / 8 / kWgThreads;
+    Chunk8<Y> y[kPassY];
+    u32x2 x[kPassX];
+    uint32_t s[kPassX];
+    uint32_t ytail, xtail, stail;
+};
+
+// Token rows j0 .. of a run from `base`, `left` of them to the end, `row` bytes
+// each of which the first `width` are the tile's: loads past them give zeros
+// and touch no memory, whatever the rows' number.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t step_rows(const void* base, int64_t j0,
+                                                            int64_t left, int64_t row,
+                                                            int64_t width) {
+    const int64_t rows = left - j0 < kStepT ? left - j0 : kStepT;
+    const int64_t bytes = rows > 0 ? (rows - 1) * row + width : 0;
+    return __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(static_cast<const uint8_t*>(base) + j0 * row), (short)0,
+        (int)bytes, kBufferRaw);
+}
+// An offset past every row, also with a row's offset added: 32 rows are below
+// 2^31 bytes (checked at the entry point).
+constexpr uint32_t kNowhere = 0x80000000u;
+
+// A workgroup of 4 wavefronts (2 x 2) owns a TO x TH tile of D over a run of
+// tokens.  TAILS: o or h is not a multiple of 8.
+template <class Y, class G, int TO, int TH, bool TAILS>
+__device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan& g) {
     typedef typename Y::T YT;
     typedef typename G::T GT;
-    __shared__ float ys[kWT][kWT], xs[kWT][kWT];
-    const int64_t to = (p.o + kWT - 1) / kWT, th = (p.h + kWT - 1) / kWT;
-    for (int64_t w = blockIdx.x; w < p.n * to * th; w += gridDim.x) {
-        const int i = (int)(w / (to * th));
-        const int64_t o0 = (w / th % to) * kWT, h0 = (w % th) * kWT;
-        const int64_t m = batch_len(p.lengths, i, p.t);
-        const int tx = threadIdx.x % kWT, ty = threadIdx.x / kWT;  // 32 x 8
-        float acc[4] = {};
-        for (int64_t j0 = 0; j0 < m; j0 += kWT) {
-            for (int a = ty; a < kWT; a += 8) {
-                const int64_t j = j0 + a, tk = i * p.t + j;
-                const bool in = j < m;
-                ys[a][tx] = in && o0 + tx < p.o
-                                ? widen(static_cast<const YT*>(p.dy.p)[tk * p.dy.ld + o0 + tx])
-                                : 0.0f;
-                xs[a][tx] = in && h0 + tx < p.h
-                                ? e4m3_value(p.x.q[tk * p.x.ld_q + h0 + tx],
-                                             p.x.s[tk * p.x.ld_s + (h0 + tx) / kActGroup])
-                                : 0.0f;
-            }
-            __syncthreads();
-            for (int a = 0; a < kWT; ++a)
-                for (int b = 0; b < 4; ++b)
-                    acc[b] = __builtin_fmaf(ys[a][ty + 8 * b], xs[a][tx], acc[b]);
-            __syncthreads();
+    constexpr int NI = TO / 64, MI = TH / 64;  // 32 x 32 products of a wavefront
+    constexpr int kTerms = sizeof(YT) == 4 ? 3 : 1;
+    constexpr int kRowY = TO * 2, kRowX = TH * 2;  // bytes of a tile row
+    constexpr int kStageY = kStepT * kRowY, kStageX = kStepT * kRowX;
+    typedef Staged<Y, TO, TH> Stage;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kStages * (kStageY + kStageX)];
+
+    // workgroup -> (run, worker, tile): consecutive workgroups go to the 8
+    // dies in turn; each die takes a contiguous run of tiles, 4 x k blocks of
+    // them, whose rows and columns its L2 then holds
+    const int64_t per_unit = g.tiles_o * g.tiles_h;
+    const int64_t total = per_unit * p.n * g.splits;
+    const int64_t b = blockIdx.x, die = b % 8, each = total / 8, more = total % 8;
+    const int64_t lin = die * each + (die < more ? die : more) + b / 8;
+    const int64_t unit = lin / per_unit, tile = lin - unit * per_unit;
+    const int i = (int)(unit % p.n), split = (int)(unit / p.n);
+    const int64_t band = tile / (4 * g.tiles_h), in = tile - band * 4 * g.tiles_h;
+    const int64_t height = g.tiles_o - band * 4 < 4 ? g.tiles_o - band * 4 : 4;
+    const int64_t o0 = (band * 4 + in % height) * TO, h0 = in / height * TH;
+
+    const int64_t m = batch_len(p.lengths, i, p.t);
+    const int64_t t0 = split * g.split_t;
+    const int64_t t1 = t0 + g.split_t < m ? t0 + g.split_t : m;
+    // an even number; loads past the run's end give zeros
+    const int steps = t1 > t0 ? ((int)((t1 - t0 + kStepT - 1) / kStepT) * kTerms + 1) / 2 * 2 : 0;
+
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    // staging: thread -> token row and 8 columns; the columns past the last
+    // whole 8 of the tile's width go one to a thread
+    const int64_t left = t1 - t0;
+    const int ywidth = (int)(p.o - o0 < TO ? p.o - o0 : TO);
+    const int xwidth = (int)(p.h - h0 < TH ? p.h - h0 : TH);
+    const int64_t yld = p.dy.ld * (int)sizeof(YT), xld = p.x.ld_q, sld = p.x.ld_s;
+    const YT* ybase = static_cast<const YT*>(p.dy.p) + (i * p.t + t0) * p.dy.ld + o0;
+    const uint8_t* xbase = p.x.q + (i * p.t + t0) * xld + h0;
+    const uint8_t* sbase = p.x.s + (i * p.t + t0) * sld + h0 / kActGroup;
+    const int yrow = tid / (TO / 8), ycol = tid % (TO / 8) * 8;
+    const int xrow = tid / (TH / 8), xcol = tid % (TH / 8) * 8;
+    const uint32_t yat = ycol + 8 <= ywidth ? yrow * (uint32_t)yld + ycol * (int)sizeof(YT) : kNowhere;
+    const uint32_t xat = xcol + 8 <= xwidth ? xrow * (uint32_t)xld + xcol : kNowhere;
+    const uint32_t sat = xcol + 8 <= xwidth ? xrow * (uint32_t)sld + xcol / kActGroup : kNowhere;
+    const bool ysplit = TAILS && ywidth % 8 != 0, xsplit = TAILS && xwidth % 8 != 0;
+    const int trow = tid / 8, ytcol = ywidth / 8 * 8 + tid % 8, xtcol = xwidth / 8 * 8 + tid % 8;
+    const uint32_t ytat = ytcol < ywidth ? trow * (uint32_t)yld + ytcol * (int)sizeof(YT) : kNowhere;
+    const uint32_t xtat = xtcol < xwidth ? trow * (uint32_t)xld + xtcol : kNowhere;
+    const uint32_t stat = xtcol < xwidth ? trow * (uint32_t)sld + xtcol / kActGroup : kNowhere;
+    const bool ywhole = !(ysplit && ycol == ywidth / 8 * 8);
+    const bool xwhole = !(xsplit && xcol == xwidth / 8 * 8);
+
+    auto load_stage = [&](Stage& r, int step) {
+        const int64_t j0 = (int64_t)(step / kTerms) * kStepT;
+        const auto yr = step_rows(ybase, j0, left, yld, ywidth * (int)sizeof(YT));
+        const auto xr = step_rows(xbase, j0, left, xld, xwidth);
+        const auto sr = step_rows(sbase, j0, left, sld, (xwidth + kActGroup - 1) / kActGroup);
+#pragma unroll
+        for (int a = 0; a < Stage::kPassY; ++a)
+            r.y[a].load(yr, yat + (uint32_t)(a * (kStepT / Stage::kPassY)) * (uint32_t)yld);
+#pragma unroll
+        for (int a = 0; a < Stage::kPassX; ++a) {
+            const uint32_t row = a * (kStepT / Stage::kPassX);
+            r.x[a] = __builtin_amdgcn_raw_buffer_load_b64(xr, xat + row * (uint32_t)xld, 0, 0);
+            r.s[a] = __builtin_amdgcn_raw_buffer_load_b8(sr, sat + row * (uint32_t)sld, 0, 0);
         }
-        GT* dst = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset;
-        for (int b = 0; b < 4; ++b) {
-            const int64_t r = o0 + ty + 8 * b, c = h0 + tx;
-            if (r >= p.o || c >= p.h) continue;
-            GT* d = dst + r * p.h + c;
-            *d = narrow<GT>(p.accumulate ? __builtin_fmaf(p.scale, acc[b], widen(*d))
-                                         : p.scale * acc[b]);
+        if (ysplit) r.ytail = Chunk8<Y>::load1(yr, ytat);
+        if (xsplit) {
+            r.xtail = __builtin_amdgcn_raw_buffer_load_b8(xr, xtat, 0, 0);
+            r.stail = __builtin_amdgcn_raw_buffer_load_b8(sr, stat, 0, 0);
         }
+    };
+    auto store_stage = [&](const Stage& r, int step) {
+        uint8_t* ys = lds + step % kStages * (kStageY + kStageX);
+        uint8_t* xs = ys + kStageY;
+        auto place = [](int k, int col, int row_bytes) {
+            return k * row_bytes + unit_at(k, col / 16) * 32 + col % 16 * 2;
+        };
+#pragma unroll
+        for (int a = 0; a < Stage::kPassY; ++a) {
+            const int k = yrow + a * (kStepT / Stage::kPassY);
+            if (ywhole)
+                *reinterpret_cast<u32x4*>(ys + place(k, ycol, kRowY)) = r.y[a].terms(step % kTerms);
+        }
+#pragma unroll
+        for (int a = 0; a < Stage::kPassX; ++a) {
+            const int k = xrow + a * (kStepT / Stage::kPassX);
+            if (xwhole)
+                *reinterpret_cast<u32x4*>(xs + place(k, xcol, kRowX)) = restore8(r.x[a], r.s[a]);
+        }
+        if (ysplit)
+            *reinterpret_cast<uint16_t*>(ys + place(trow, ytcol, kRowY)) =
+                (uint16_t)Chunk8<Y>::term1(r.ytail, step % kTerms);
+        if (xsplit)
+            *reinterpret_cast<uint16_t*>(xs + place(trow, xtcol, kRowX)) =
+                (uint16_t)restore8(u32x2{r.xtail, 0}, r.stail).x;
+    };
+    auto barrier = [] {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    };
+
+    // fragments: lane -> column l % 32 of a 32-column block, 8 tokens.  16
+    // lanes read 4 token rows x 16 columns, 8 bytes each, and get a column each.
+    const int wo = wave / 2 * (TO / 2), wh = wave % 2 * (TH / 2);
+    const int frow = (lane / 32) * 8 + lane % 16 / 4;  // and + 4 for the second read
+    int yaddr[NI], xaddr[MI];
+#pragma unroll
+    for (int a = 0; a < NI; ++a)
+        yaddr[a] = frow * kRowY + unit_at(frow, (wo + a * 32) / 16 + lane / 16 % 2) * 32 +
+                   lane % 4 * 8;
+#pragma unroll
+    for (int a = 0; a < MI; ++a)
+        xaddr[a] = kStageY + frow * kRowX +
+                   unit_at(frow, (wh + a * 32) / 16 + lane / 16 % 2) * 32 + lane % 4 * 8;
+    auto fragment = [&](int at, int row_bytes) {
+        uint8_t* q = lds + at;
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad*)q);
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad*)(q + 4 * row_bytes));
+        bf16x8 f;
+        __builtin_memcpy(&f, &lo, 8);
+        __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
+        return f;
+    };
+    struct Frags {
+        bf16x8 y[NI], x[MI];
+    };
+    auto read_frags = [&](Frags& f, int step, int half) {
+        const int base = step % kStages * (kStageY + kStageX);
+#pragma unroll
+        for (int a = 0; a < NI; ++a) f.y[a] = fragment(base + yaddr[a] + half * 16 * kRowY, kRowY);
+#pragma unroll
+        for (int a = 0; a < MI; ++a) f.x[a] = fragment(base + xaddr[a] + half * 16 * kRowX, kRowX);
+    };
+    f32x16 acc[MI][NI] = {};
+    auto multiply = [&](const Frags& f) {
+#pragma unroll
+        for (int a = 0; a < MI; ++a)
+#pragma unroll
+            for (int c = 0; c < NI; ++c)
+                acc[a][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.x[a], f.y[c], acc[a][c], 0,
+                                                                    0, 0);
+    };
+
+    // Step s multiplies tile s, stores tile s + 2 (whose place was last read in
+    // step s - 1) and loads tile s + 4 into the registers this frees; the first
+    // fragments of tile s + 1 are read at the end, so that the matrix units
+    // have work while the workgroup meets.
+    Stage r[2];
+    Frags f0, f1;
+    load_stage(r[0], 0);
+    load_stage(r[1], 1);
+    store_stage(r[0], 0);
+    load_stage(r[0], 2);
+    store_stage(r[1], 1);
+    load_stage(r[1], 3);
+    barrier();
+    read_frags(f0, 0, 0);
+    auto step = [&](Stage& reg, int s) {
+        read_frags(f1, s, 1);
+        multiply(f0);
+        store_stage(reg, s + 2);
+        load_stage(reg, s + 4);
+        read_frags(f0, s + 1, 0);
+        multiply(f1);
+        barrier();
+    };
+    for (int s = 0; s < steps; s += 2) {
+        step(r[0], s);
+        step(r[1], s + 1);
     }
+
+    // lane -> column (output row) o, 4 x 4 consecutive h
+#pragma unroll
+    for (int a = 0; a < MI; ++a)
+#pragma unroll
+        for (int c = 0; c < NI; ++c) {
+            const int64_t o = o0 + wo + c * 32 + lane % 32;
+            if (o >= p.o) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t h = h0 + wh + a * 32 + e * 8 + lane / 32 * 4;
+                const int64_t have = p.h - h;
+                if (have <= 0) continue;
+                float v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = acc[a][c][e * 4 + k];
+                if (g.splits > 1) {
+                    store_unit<float, 4, false>(
+                        g.part + (((int64_t)split * p.n + i) * p.o + o) * p.h + h, have, v);
+                    continue;
+                }
+                GT* d = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + o * p.h + h;
+                float old[4];
+                if (p.accumulate) load_unit<GT, 4, false>(d, have, old);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    v[k] = p.accumulate ? __builtin_fmaf(p.scale, v[k], old[k]) : p.scale * v[k];
+                store_unit<GT, 4, false>(d, have, v);
+            }
+        }
+}
+
+template <class Y, class G>
+__global__ __launch_bounds__(kWgThreads, 1) void k_act_wgrad_256(WgradParams p, WgradPlan g) {
+    wgrad_tile<Y, G, 256, 256, false>(p, g);
+}
+
+template <class Y, class G>
+__global__ __launch_bounds__(kWgThreads, 2) void k_act_wgrad_128(WgradParams p, WgradPlan g) {
+    wgrad_tile<Y, G, 128, 128, true>(p, g);
+}
+
+// Sum of the runs' partial results, in order.
+template <class G>
+__global__ __launch_bounds__(kBlock) void k_act_wgrad_join(WgradParams p, WgradPlan g) {
+    typedef typename G::T GT;
+    const int64_t size = p.o * p.h, units = (size + 3) / 4, total = units * p.n;
+    for (int64_t w = (int64_t)blockIdx.x * kBlock + threadIdx.x; w < total;
+         w += (int64_t)gridDim.x * kBlock) {
+        const int64_t i = w / units, c = (w - i * units) * 4, have = size - c;
+        float sum[4] = {};
+        for (int s = 0; s < g.splits; ++s) {
+            float v[4];
+            load_unit<float, 4, false>(g.part + ((int64_t)s * p.n + i) * size + c, have, v);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] += v[k];
+        }
+        GT* d = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + c;
+        float old[4];
+        if (p.accumulate) load_unit<GT, 4, false>(d, have, old);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            sum[k] = p.accumulate ? __builtin_fmaf(p.scale, sum[k], old[k]) : p.scale * sum[k];
+        store_unit<GT, 4, false>(d, have, sum);
+    }
+}
+
+constexpr int kCus = 256;
+
+// Tile edge and token runs.  256 x 256 tiles where they give every compute unit
+// one (and both widths are multiples of 8), else 128 x 128; where even those are fewer than the compute units, the
+// tokens are cut into runs of at least 8 steps.
+int wgrad_plan(int64_t n, int64_t t, int64_t o, int64_t h, WgradPlan* g) {
+    auto tiles = [&](int64_t e) { return n * ((o + e - 1) / e) * ((h + e - 1) / e); };
+    const int edge = tiles(256) >= kCus && o % 8 == 0 && h % 8 == 0 ? 256 : 128;
+    g->tiles_o = (o + edge - 1) / edge;
+    g->tiles_h = (h + edge - 1) / edge;
+    const int64_t steps = (t + kStepT - 1) / kStepT;
+    int64_t splits = 1;
+    if (tiles(edge) < kCus) {
+        splits = (2 * kCus) / tiles(edge);
+        const int64_t most = steps / 8;
+        splits = splits < most ? splits : most;
+        if (splits < 1) splits = 1;
+    }
+    const int64_t each = (steps + splits - 1) / splits;
+    g->split_t = (each < 1 ? 1 : each) * kStepT;
+    g->splits = (int)(each < 1 ? 1 : (steps + each - 1) / each);
+    return edge;
 }
 
 }  // namespace
 
-size_t act_wgrad_workspace(int64_t, int64_t, int64_t, int64_t) { return 0; }
+size_t act_wgrad_workspace(int64_t n, int64_t t, int64_t o, int64_t h) {
+    WgradPlan g;
+    wgrad_plan(n, t, o, h, &g);
+    return g.splits > 1 ? (size_t)g.splits * n * o * h * 4 : 0;
+}
 
-hipError_t launch_act_wgrad(const WgradParams& p, void*, hipStream_t s) {
-    const dim3 grid(grid_for(p.n * ((p.o + kWT - 1) / kWT) * ((p.h + kWT - 1) / kWT)));
-    LOSSY_LAUNCH2(k_act_wgrad, p.dy.bf16, p.grads.bf16, grid, dim3(kBlock), s, p);
+hipError_t launch_act_wgrad(const WgradParams& p, void* ws, hipStream_t s) {
+    WgradPlan g;
+    const int edge = wgrad_plan(p.n, p.t, p.o, p.h, &g);
+    g.part = static_cast<float*>(ws);
+    const int64_t blocks = g.tiles_o * g.tiles_h * p.n * g.splits;
+    if (blocks > 0xFFFFFFFFll / kWgThreads) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks);
+    if (edge == 256)
+        LOSSY_LAUNCH2(k_act_wgrad_256, p.dy.bf16, p.grads.bf16, grid, dim3(kWgThreads), s, p, g);
+    else
+        LOSSY_LAUNCH2(k_act_wgrad_128, p.dy.bf16, p.grads.bf16, grid, dim3(kWgThreads), s, p, g);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || g.splits == 1) return e;
+    const dim3 join(grid_for((p.n * ((p.o * p.h + 3) / 4) + kBlock - 1) / kBlock));
+    if (p.grads.bf16)
+        hipLaunchKernelGGL((k_act_wgrad_join<El16>), join, dim3(kBlock), 0, s, p, g);
+    else
+        hipLaunchKernelGGL((k_act_wgrad_join<El32>), join, dim3(kBlock), 0, s, p, g);
     return hipGetLastError();
 }
 

@@ -374,6 +374,10 @@ WGRAD = [
     (4, 31, 8, 2056, BF16, BF16, 16, None, 0, 0, 0, 0),
     (1, 5000, 96, 160, BF16, BF16, 0, [4097], 0, 0, 0, 0),
     (1, 96, 515, 300, F32, BF16, 2, None, 0, 0, 0, 2),
+    # as many tiles as compute units and more
+    (66, 75, 264, 520, BF16, BF16, 3, [75, 0, 33] * 22, 8, 8, 0, 0),
+    (65, 41, 512, 264, F32, F32, 0, None, 1, 1, 1, 1),
+    (67, 1, 520, 272, BF16, F32, 1, [1, 0] * 33 + [1], 0, 3, 0, 1),
 ]
 
 
@@ -421,7 +425,9 @@ def test_act_wgrad(n, t, o, h, ydt, gdt, offset, lens, py, pq, ps, shift, accumu
 
 @pytest.mark.parametrize("ydt,top", [(BF16, 8), (F32, 500)])
 @pytest.mark.parametrize("n,t,o,h", [(1, 4096, 256, 256), (2, 1000, 520, 264), (1, 9001, 65, 40),
-                                     (3, 130, 770, 1030), (1, 700, 1025, 2049)])
+                                     (3, 130, 770, 1030), (1, 700, 1025, 2049),
+                                     (70, 37, 264, 520), (1, 290, 4096, 4104),
+                                     (256, 100, 40, 16)])
 def test_act_wgrad_whole_numbers_are_exact(n, t, o, h, ydt, top):
     # |x| <= 3 and |dy| <= top: every partial sum is below 9001 * 3 * 500 < 2^24
     dy = ints((n, t, o), -top, top, 14, ydt)
