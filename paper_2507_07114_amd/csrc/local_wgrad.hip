@@ -23,8 +23,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) i16x4 LdsQuad;
 
 constexpr int kStepT = 32;    // tokens of a step
-constexpr int kStages = 3;    // steps whose tiles are in LDS
-constexpr int kWgThreads = 256;
+constexpr int kStages = 4;    // steps whose tiles are in LDS, as two pairs
 
 struct WgradPlan {
     int64_t tiles_o, tiles_h;
@@ -39,19 +38,23 @@ struct WgradPlan {
 // 16 lanes' fall on different banks.
 __device__ __forceinline__ int unit_at(int k, int unit) { return unit ^ (2 * (k & 3)); }
 
-// The bf16 terms of an fp32 value: the leading 8 significant bits, the next 8
-// and the rest, each cut off (so that every difference is exact).  What is
-// not finite has one term.
-__device__ __forceinline__ uint32_t f32_term(float x, int part) {
-    const uint32_t u = __float_as_uint(x);
-    const uint32_t hi = u & 0xFFFF0000u;
-    if ((u & 0x7F800000u) == 0x7F800000u)
-        return part ? 0u : (u & 0x7FFFFFu ? 0x7FC0u : hi >> 16);
-    if (part == 0) return hi >> 16;
-    const float r = x - __uint_as_float(hi);
-    const uint32_t mid = __float_as_uint(r) & 0xFFFF0000u;
-    if (part == 1) return mid >> 16;
-    return __float_as_uint(r - __uint_as_float(mid)) >> 16;
+// Two fp32 values' bf16 term PART side by side: the leading 8 significant bits,
+// the next 8 and the rest, each cut off, so that every difference is exact.  An
+// infinite value has only the first; a NaN is one in the others.
+template <int PART>
+__device__ __forceinline__ uint32_t f32_terms(uint32_t lo, uint32_t hi) {
+    auto rest = [](uint32_t u) {  // what the first PART terms leave
+        float x = __uint_as_float(u);
+        const float r = x - __uint_as_float(u & 0xFFFF0000u);
+        x = __builtin_isinf(x) ? 0.0f : r;
+        if (PART == 2) x -= __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+        return __float_as_uint(x);
+    };
+    if (PART > 0) {
+        lo = rest(lo);
+        hi = rest(hi);
+    }
+    return __builtin_amdgcn_perm(hi, lo, 0x07060302);  // the upper halves
 }
 
 // 8 columns of dy of one token, and one column.
@@ -63,11 +66,17 @@ struct Chunk8<El16> {
     __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
         a = __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
     }
-    __device__ __forceinline__ u32x4 terms(int) const { return a; }
+    template <int PART>
+    __device__ __forceinline__ u32x4 terms() const {
+        return a;
+    }
     static __device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t r, uint32_t at) {
         return __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
     }
-    static __device__ __forceinline__ uint32_t term1(uint32_t x, int) { return x; }
+    template <int PART>
+    static __device__ __forceinline__ uint32_t term1(uint32_t x) {
+        return x;
+    }
 };
 template <>
 struct Chunk8<El32> {
@@ -76,17 +85,17 @@ struct Chunk8<El32> {
         a = __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
         b = __builtin_amdgcn_raw_buffer_load_b128(r, at + 16, 0, 0);
     }
-    __device__ __forceinline__ u32x4 terms(int part) const {
-        auto two = [&](uint32_t lo, uint32_t hi) {
-            return f32_term(__uint_as_float(lo), part) | f32_term(__uint_as_float(hi), part) << 16;
-        };
-        return u32x4{two(a.x, a.y), two(a.z, a.w), two(b.x, b.y), two(b.z, b.w)};
+    template <int PART>
+    __device__ __forceinline__ u32x4 terms() const {
+        return u32x4{f32_terms<PART>(a.x, a.y), f32_terms<PART>(a.z, a.w),
+                     f32_terms<PART>(b.x, b.y), f32_terms<PART>(b.z, b.w)};
     }
     static __device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t r, uint32_t at) {
         return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
     }
-    static __device__ __forceinline__ uint32_t term1(uint32_t x, int part) {
-        return f32_term(__uint_as_float(x), part);
+    template <int PART>
+    static __device__ __forceinline__ uint32_t term1(uint32_t x) {
+        return f32_terms<PART>(x, 0);
     }
 };
 
@@ -105,44 +114,46 @@ __device__ __forceinline__ u32x4 restore8(u32x2 code, uint32_t s) {
 
 // Staging registers of one step of one thread: 8 columns of kPass token rows,
 // and an element of the columns past the last whole 8.
-template <class Y, int TO, int TH>
+template <class Y, int TO, int TH, int THREADS>
 struct Staged {
-    static constexpr int kPassY = kStepT * TO / 8 / kWgThreads;
-    static constexpr int kPassX = kStepT * TH / 8 / kWgThreads;
+    static constexpr int kPassY = kStepT * TO / 8 / THREADS;
+    static constexpr int kPassX = kStepT * TH / 8 / THREADS;
     Chunk8<Y> y[kPassY];
     u32x2 x[kPassX];
     uint32_t s[kPassX];
     uint32_t ytail, xtail, stail;
 };
 
-// Token rows j0 .. of a run from `base`, `left` of them to the end, `row` bytes
-// each of which the first `width` are the tile's: loads past them give zeros
-// and touch no memory, whatever the rows' number.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t step_rows(const void* base, int64_t j0,
-                                                            int64_t left, int64_t row,
-                                                            int64_t width) {
-    const int64_t rows = left - j0 < kStepT ? left - j0 : kStepT;
-    const int64_t bytes = rows > 0 ? (rows - 1) * row + width : 0;
-    return __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(static_cast<const uint8_t*>(base) + j0 * row), (short)0,
-        (int)bytes, kBufferRaw);
+// The next `rows` (0 to 32) token rows at p, `row` bytes each of which the first
+// `width` are the tile's: loads past them give zeros and touch no memory.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t step_rows(const uint8_t* p, int rows, int row,
+                                                            int width) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0,
+                                             rows > 0 ? (rows - 1) * row + width : 0, kBufferRaw);
 }
 // An offset past every row, also with a row's offset added: 32 rows are below
 // 2^31 bytes (checked at the entry point).
 constexpr uint32_t kNowhere = 0x80000000u;
 
-// A workgroup of 4 wavefronts (2 x 2) owns a TO x TH tile of D over a run of
+template <int N>
+struct Part {
+    static constexpr int value = N;
+};
+
+// A workgroup of WO x WH wavefronts owns a TO x TH tile of D over a run of
 // tokens.  TAILS: o or h is not a multiple of 8.
-template <class Y, class G, int TO, int TH, bool TAILS>
+template <class Y, class G, int TO, int TH, int WO, int WH, bool TAILS>
 __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan& g) {
     typedef typename Y::T YT;
     typedef typename G::T GT;
-    constexpr int NI = TO / 64, MI = TH / 64;  // 32 x 32 products of a wavefront
+    constexpr int kThreads = WO * WH * kWave;
+    constexpr int NI = TO / WO / 32, MI = TH / WH / 32;  // 32 x 32 products of a wavefront
     constexpr int kTerms = sizeof(YT) == 4 ? 3 : 1;
     constexpr int kRowY = TO * 2, kRowX = TH * 2;  // bytes of a tile row
     constexpr int kStageY = kStepT * kRowY, kStageX = kStepT * kRowX;
-    typedef Staged<Y, TO, TH> Stage;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kStages * (kStageY + kStageX)];
+    constexpr int kStage = kStageY + kStageX, kPair = 2 * kStage;  // powers of two
+    typedef Staged<Y, TO, TH, kThreads> Stage;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kStages * kStage];
 
     // workgroup -> (run, worker, tile): consecutive workgroups go to the 8
     // dies in turn; each die takes a contiguous run of tiles, 4 x k blocks of
@@ -160,37 +171,46 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     const int64_t m = batch_len(p.lengths, i, p.t);
     const int64_t t0 = split * g.split_t;
     const int64_t t1 = t0 + g.split_t < m ? t0 + g.split_t : m;
-    // an even number; loads past the run's end give zeros
-    const int steps = t1 > t0 ? ((int)((t1 - t0 + kStepT - 1) / kStepT) * kTerms + 1) / 2 * 2 : 0;
+    // tokens in pairs of blocks; loads past the run's end give zeros
+    const int left = t1 > t0 ? (int)(t1 - t0) : 0;
+    const int pairs = (left + 2 * kStepT - 1) / (2 * kStepT);
 
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     // staging: thread -> token row and 8 columns; the columns past the last
     // whole 8 of the tile's width go one to a thread
-    const int64_t left = t1 - t0;
     const int ywidth = (int)(p.o - o0 < TO ? p.o - o0 : TO);
     const int xwidth = (int)(p.h - h0 < TH ? p.h - h0 : TH);
-    const int64_t yld = p.dy.ld * (int)sizeof(YT), xld = p.x.ld_q, sld = p.x.ld_s;
-    const YT* ybase = static_cast<const YT*>(p.dy.p) + (i * p.t + t0) * p.dy.ld + o0;
-    const uint8_t* xbase = p.x.q + (i * p.t + t0) * xld + h0;
-    const uint8_t* sbase = p.x.s + (i * p.t + t0) * sld + h0 / kActGroup;
+    const int yld = (int)p.dy.ld * (int)sizeof(YT), xld = (int)p.x.ld_q, sld = (int)p.x.ld_s;
+    const uint8_t* ynext = reinterpret_cast<const uint8_t*>(
+        static_cast<const YT*>(p.dy.p) + (i * p.t + t0) * p.dy.ld + o0);
+    const uint8_t* xnext = p.x.q + (i * p.t + t0) * p.x.ld_q + h0;
+    const uint8_t* snext = p.x.s + (i * p.t + t0) * p.x.ld_s + h0 / kActGroup;
+    int rows_left = left;  // from the next step's first token on
     const int yrow = tid / (TO / 8), ycol = tid % (TO / 8) * 8;
     const int xrow = tid / (TH / 8), xcol = tid % (TH / 8) * 8;
     const uint32_t yat = ycol + 8 <= ywidth ? yrow * (uint32_t)yld + ycol * (int)sizeof(YT) : kNowhere;
     const uint32_t xat = xcol + 8 <= xwidth ? xrow * (uint32_t)xld + xcol : kNowhere;
     const uint32_t sat = xcol + 8 <= xwidth ? xrow * (uint32_t)sld + xcol / kActGroup : kNowhere;
     const bool ysplit = TAILS && ywidth % 8 != 0, xsplit = TAILS && xwidth % 8 != 0;
-    const int trow = tid / 8, ytcol = ywidth / 8 * 8 + tid % 8, xtcol = xwidth / 8 * 8 + tid % 8;
+    const int trow = tid / 8 % kStepT, ytcol = ywidth / 8 * 8 + tid % 8, xtcol = xwidth / 8 * 8 + tid % 8;
     const uint32_t ytat = ytcol < ywidth ? trow * (uint32_t)yld + ytcol * (int)sizeof(YT) : kNowhere;
     const uint32_t xtat = xtcol < xwidth ? trow * (uint32_t)xld + xtcol : kNowhere;
     const uint32_t stat = xtcol < xwidth ? trow * (uint32_t)sld + xtcol / kActGroup : kNowhere;
     const bool ywhole = !(ysplit && ycol == ywidth / 8 * 8);
     const bool xwhole = !(xsplit && xcol == xwidth / 8 * 8);
 
-    auto load_stage = [&](Stage& r, int step) {
-        const int64_t j0 = (int64_t)(step / kTerms) * kStepT;
-        const auto yr = step_rows(ybase, j0, left, yld, ywidth * (int)sizeof(YT));
-        const auto xr = step_rows(xbase, j0, left, xld, xwidth);
-        const auto sr = step_rows(sbase, j0, left, sld, (xwidth + kActGroup - 1) / kActGroup);
+    // the tiles of the next step; its tokens are done with `last`
+    auto load_stage = [&](Stage& r, bool last) {
+        const int rows = rows_left < kStepT ? rows_left : kStepT;
+        const auto yr = step_rows(ynext, rows, yld, ywidth * (int)sizeof(YT));
+        const auto xr = step_rows(xnext, rows, xld, xwidth);
+        const auto sr = step_rows(snext, rows, sld, (xwidth + kActGroup - 1) / kActGroup);
+        if (last) {
+            ynext += (int64_t)kStepT * yld;
+            xnext += (int64_t)kStepT * xld;
+            snext += (int64_t)kStepT * sld;
+            rows_left -= kStepT;
+        }
 #pragma unroll
         for (int a = 0; a < Stage::kPassY; ++a)
             r.y[a].load(yr, yat + (uint32_t)(a * (kStepT / Stage::kPassY)) * (uint32_t)yld);
@@ -206,29 +226,36 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
             r.stail = __builtin_amdgcn_raw_buffer_load_b8(sr, stat, 0, 0);
         }
     };
-    auto store_stage = [&](const Stage& r, int step) {
-        uint8_t* ys = lds + step % kStages * (kStageY + kStageX);
-        uint8_t* xs = ys + kStageY;
-        auto place = [](int k, int col, int row_bytes) {
-            return k * row_bytes + unit_at(k, col / 16) * 32 + col % 16 * 2;
-        };
+    // LDS places of what a thread stages, in the current pair of stages; a
+    // change of pair flips one bit
+    auto place = [](int k, int col, int row_bytes) {
+        return k * row_bytes + unit_at(k, col / 16) * 32 + col % 16 * 2;
+    };
+    int yput[Stage::kPassY], xput[Stage::kPassX];
 #pragma unroll
-        for (int a = 0; a < Stage::kPassY; ++a) {
-            const int k = yrow + a * (kStepT / Stage::kPassY);
-            if (ywhole)
-                *reinterpret_cast<u32x4*>(ys + place(k, ycol, kRowY)) = r.y[a].terms(step % kTerms);
-        }
+    for (int a = 0; a < Stage::kPassY; ++a)
+        yput[a] = place(yrow + a * (kStepT / Stage::kPassY), ycol, kRowY);
 #pragma unroll
-        for (int a = 0; a < Stage::kPassX; ++a) {
-            const int k = xrow + a * (kStepT / Stage::kPassX);
-            if (xwhole)
-                *reinterpret_cast<u32x4*>(xs + place(k, xcol, kRowX)) = restore8(r.x[a], r.s[a]);
-        }
+    for (int a = 0; a < Stage::kPassX; ++a)
+        xput[a] = kStageY + place(xrow + a * (kStepT / Stage::kPassX), xcol, kRowX);
+    int ytput = place(trow, ytcol, kRowY), xtput = kStageY + place(trow, xtcol, kRowX);
+    // store into the pair that `pair` says (0 or kPair), its stage `half`
+    auto store_stage = [&](const Stage& r, auto part, int pair, int half) {
+        constexpr int kPart = decltype(part)::value;
+        uint8_t* to = lds + half * kStage;
+#pragma unroll
+        for (int a = 0; a < Stage::kPassY; ++a)
+            if (!TAILS || ywhole)
+                *reinterpret_cast<u32x4*>(to + (yput[a] ^ pair)) = r.y[a].template terms<kPart>();
+#pragma unroll
+        for (int a = 0; a < Stage::kPassX; ++a)
+            if (!TAILS || xwhole)
+                *reinterpret_cast<u32x4*>(to + (xput[a] ^ pair)) = restore8(r.x[a], r.s[a]);
         if (ysplit)
-            *reinterpret_cast<uint16_t*>(ys + place(trow, ytcol, kRowY)) =
-                (uint16_t)Chunk8<Y>::term1(r.ytail, step % kTerms);
+            *reinterpret_cast<uint16_t*>(to + (ytput ^ pair)) =
+                (uint16_t)Chunk8<Y>::template term1<kPart>(r.ytail);
         if (xsplit)
-            *reinterpret_cast<uint16_t*>(xs + place(trow, xtcol, kRowX)) =
+            *reinterpret_cast<uint16_t*>(to + (xtput ^ pair)) =
                 (uint16_t)restore8(u32x2{r.xtail, 0}, r.stail).x;
     };
     auto barrier = [] {
@@ -239,7 +266,7 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
 
     // fragments: lane -> column l % 32 of a 32-column block, 8 tokens.  16
     // lanes read 4 token rows x 16 columns, 8 bytes each, and get a column each.
-    const int wo = wave / 2 * (TO / 2), wh = wave % 2 * (TH / 2);
+    const int wo = wave / WH * (TO / WO), wh = wave % WH * (TH / WH);
     const int frow = (lane / 32) * 8 + lane % 16 / 4;  // and + 4 for the second read
     int yaddr[NI], xaddr[MI];
 #pragma unroll
@@ -262,12 +289,15 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     struct Frags {
         bf16x8 y[NI], x[MI];
     };
-    auto read_frags = [&](Frags& f, int step, int half) {
-        const int base = step % kStages * (kStageY + kStageX);
+    auto read_frags = [&](Frags& f, int pair, int stage, int half) {
 #pragma unroll
-        for (int a = 0; a < NI; ++a) f.y[a] = fragment(base + yaddr[a] + half * 16 * kRowY, kRowY);
+        for (int a = 0; a < MI; ++a) {
+            f.x[a] = fragment((xaddr[a] ^ pair) + stage * kStage + half * 16 * kRowX, kRowX);
+            if (a == 0)
 #pragma unroll
-        for (int a = 0; a < MI; ++a) f.x[a] = fragment(base + xaddr[a] + half * 16 * kRowX, kRowX);
+                for (int c = 0; c < NI; ++c)
+                    f.y[c] = fragment((yaddr[c] ^ pair) + stage * kStage + half * 16 * kRowY, kRowY);
+        }
     };
     f32x16 acc[MI][NI] = {};
     auto multiply = [&](const Frags& f) {
@@ -280,31 +310,60 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     };
 
     // Step s multiplies tile s, stores tile s + 2 (whose place was last read in
-    // step s - 1) and loads tile s + 4 into the registers this frees; the first
-    // fragments of tile s + 1 are read at the end, so that the matrix units
-    // have work while the workgroup meets.
+    // step s - 2) and loads tile s + 4 into the registers this frees.  The
+    // workgroup meets in the middle of the step, with the second half's
+    // fragments already read; what it stored before is read from the next step
+    // on.  A wavefront issues an instruction every 4 cycles and a product takes
+    // 32: the groups below deal the reads, stores and loads out between the
+    // products.
     Stage r[2];
     Frags f0, f1;
-    load_stage(r[0], 0);
-    load_stage(r[1], 1);
-    store_stage(r[0], 0);
-    load_stage(r[0], 2);
-    store_stage(r[1], 1);
-    load_stage(r[1], 3);
+    load_stage(r[0], kTerms == 1);
+    load_stage(r[1], kTerms == 1);
+    store_stage(r[0], Part<0>(), 0, 0);
+    load_stage(r[0], true);
+    store_stage(r[1], Part<1 % kTerms>(), 0, 1);
+    load_stage(r[1], kTerms == 1);
     barrier();
-    read_frags(f0, 0, 0);
-    auto step = [&](Stage& reg, int s) {
-        read_frags(f1, s, 1);
+    read_frags(f0, 0, 0, 0);
+    int pair = 0;
+    constexpr int kProducts = MI * NI, kReads = 2 * (MI + NI);
+    constexpr int kReadsEach = (kReads + kProducts - 1) / kProducts;
+    // step s of 2 * kTerms: term s % kTerms of token block s / kTerms
+    auto step = [&](auto part) {
+        constexpr int s = decltype(part)::value, odd = s % 2;
+        read_frags(f1, pair, odd, 1);
+        store_stage(r[odd], Part<(s + 2) % kTerms>(), pair ^ kPair, odd);
         multiply(f0);
-        store_stage(reg, s + 2);
-        load_stage(reg, s + 4);
-        read_frags(f0, s + 1, 0);
-        multiply(f1);
+#pragma unroll
+        for (int k = 0; k < kProducts; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // product
+            __builtin_amdgcn_sched_group_barrier(0x100, kReadsEach, 0);  // LDS read
+            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);  // arithmetic
+            if (k % 2) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // LDS write
+        }
         barrier();
+        load_stage(r[odd], (s + 4) % kTerms == kTerms - 1);
+        if (odd) pair ^= kPair;
+        read_frags(f0, pair, 1 - odd, 0);
+        multiply(f1);
+#pragma unroll
+        for (int k = 0; k < kProducts; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, kReadsEach, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // load
+        }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    for (int s = 0; s < steps; s += 2) {
-        step(r[0], s);
-        step(r[1], s + 1);
+    for (int k = 0; k < pairs; ++k) {
+        step(Part<0>());
+        step(Part<1>());
+        if (kTerms == 3) {
+            step(Part<2 % (2 * kTerms)>());
+            step(Part<3 % (2 * kTerms)>());
+            step(Part<4 % (2 * kTerms)>());
+            step(Part<5 % (2 * kTerms)>());
+        }
     }
 
     // lane -> column (output row) o, 4 x 4 consecutive h
@@ -339,13 +398,13 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
 }
 
 template <class Y, class G>
-__global__ __launch_bounds__(kWgThreads, 1) void k_act_wgrad_256(WgradParams p, WgradPlan g) {
-    wgrad_tile<Y, G, 256, 256, false>(p, g);
+__global__ __launch_bounds__(512, 1) void k_act_wgrad_256(WgradParams p, WgradPlan g) {
+    wgrad_tile<Y, G, 256, 256, 2, 4, false>(p, g);
 }
 
 template <class Y, class G>
-__global__ __launch_bounds__(kWgThreads, 2) void k_act_wgrad_128(WgradParams p, WgradPlan g) {
-    wgrad_tile<Y, G, 128, 128, true>(p, g);
+__global__ __launch_bounds__(256, 2) void k_act_wgrad_128(WgradParams p, WgradPlan g) {
+    wgrad_tile<Y, G, 128, 128, 2, 2, true>(p, g);
 }
 
 // Sum of the runs' partial results, in order.
@@ -410,12 +469,12 @@ hipError_t launch_act_wgrad(const WgradParams& p, void* ws, hipStream_t s) {
     const int edge = wgrad_plan(p.n, p.t, p.o, p.h, &g);
     g.part = static_cast<float*>(ws);
     const int64_t blocks = g.tiles_o * g.tiles_h * p.n * g.splits;
-    if (blocks > 0xFFFFFFFFll / kWgThreads) return hipErrorInvalidConfiguration;
+    if (blocks > 0xFFFFFFFFll / 512) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks);
     if (edge == 256)
-        LOSSY_LAUNCH2(k_act_wgrad_256, p.dy.bf16, p.grads.bf16, grid, dim3(kWgThreads), s, p, g);
+        LOSSY_LAUNCH2(k_act_wgrad_256, p.dy.bf16, p.grads.bf16, grid, dim3(512), s, p, g);
     else
-        LOSSY_LAUNCH2(k_act_wgrad_128, p.dy.bf16, p.grads.bf16, grid, dim3(kWgThreads), s, p, g);
+        LOSSY_LAUNCH2(k_act_wgrad_128, p.dy.bf16, p.grads.bf16, grid, dim3(256), s, p, g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.splits == 1) return e;
     const dim3 join(grid_for((p.n * ((p.o * p.h + 3) / 4) + kBlock - 1) / kBlock));
