@@ -309,13 +309,12 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
                                                                     0, 0);
     };
 
-    // Step s multiplies tile s, stores tile s + 2 (whose place was last read in
-    // step s - 2) and loads tile s + 4 into the registers this frees.  The
-    // workgroup meets in the middle of the step, with the second half's
-    // fragments already read; what it stored before is read from the next step
-    // on.  A wavefront issues an instruction every 4 cycles and a product takes
-    // 32: the groups below deal the reads, stores and loads out between the
-    // products.
+    // Two steps s, s + 1 multiply one pair of stages, store tiles s + 2, s + 3 into
+    // the other and load tiles s + 4, s + 5 into the registers this frees.  The
+    // workgroup meets once, before the last quarter, whose fragments are then
+    // read: behind it the stored pair may be read and this one stored.  A
+    // wavefront issues an instruction every 4 cycles and a product takes 32: the
+    // groups below deal the reads, stores and loads out between the products.
     Stage r[2];
     Frags f0, f1;
     load_stage(r[0], kTerms == 1);
@@ -330,39 +329,36 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     constexpr int kProducts = MI * NI, kReads = 2 * (MI + NI);
     constexpr int kReadsEach = (kReads + kProducts - 1) / kProducts;
     // step s of 2 * kTerms: term s % kTerms of token block s / kTerms
-    auto step = [&](auto part) {
-        constexpr int s = decltype(part)::value, odd = s % 2;
-        read_frags(f1, pair, odd, 1);
-        store_stage(r[odd], Part<(s + 2) % kTerms>(), pair ^ kPair, odd);
-        multiply(f0);
+    auto half = [&](const Frags& now, auto... after) {
+        (after(), ...);
+        multiply(now);
 #pragma unroll
         for (int k = 0; k < kProducts; ++k) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // product
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);           // product
             __builtin_amdgcn_sched_group_barrier(0x100, kReadsEach, 0);  // LDS read
-            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);  // arithmetic
-            if (k % 2) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // LDS write
-        }
-        barrier();
-        load_stage(r[odd], (s + 4) % kTerms == kTerms - 1);
-        if (odd) pair ^= kPair;
-        read_frags(f0, pair, 1 - odd, 0);
-        multiply(f1);
-#pragma unroll
-        for (int k = 0; k < kProducts; ++k) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, kReadsEach, 0);
-            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // load
+            __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);           // LDS write
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);           // load
         }
         __builtin_amdgcn_sched_barrier(0);
     };
+    auto two_steps = [&](auto part) {
+        constexpr int s = decltype(part)::value;
+        half(f0, [&] { read_frags(f1, pair, 0, 1); },
+             [&] { store_stage(r[0], Part<(s + 2) % kTerms>(), pair ^ kPair, 0); });
+        half(f1, [&] { read_frags(f0, pair, 1, 0); },
+             [&] { load_stage(r[0], (s + 4) % kTerms == kTerms - 1); });
+        half(f0, [&] { read_frags(f1, pair, 1, 1); },
+             [&] { store_stage(r[1], Part<(s + 3) % kTerms>(), pair ^ kPair, 1); });
+        barrier();
+        pair ^= kPair;
+        half(f1, [&] { read_frags(f0, pair, 0, 0); },
+             [&] { load_stage(r[1], (s + 5) % kTerms == kTerms - 1); });
+    };
     for (int k = 0; k < pairs; ++k) {
-        step(Part<0>());
-        step(Part<1>());
+        two_steps(Part<0>());
         if (kTerms == 3) {
-            step(Part<2 % (2 * kTerms)>());
-            step(Part<3 % (2 * kTerms)>());
-            step(Part<4 % (2 * kTerms)>());
-            step(Part<5 % (2 * kTerms)>());
+            two_steps(Part<2>());
+            two_steps(Part<4>());
         }
     }
 
