@@ -199,32 +199,43 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     const bool ywhole = !(ysplit && ycol == ywidth / 8 * 8);
     const bool xwhole = !(xsplit && xcol == xwidth / 8 * 8);
 
-    // the tiles of the next step; its tokens are done with `last`
-    auto load_stage = [&](Stage& r, bool last) {
+    // Loads of the next step's tiles, one piece a call (y rows, then x rows);
+    // the step's tokens are done with `last`.
+    __amdgpu_buffer_rsrc_t yr, xr, sr;
+    auto open_stage = [&](bool last) {
         const int rows = rows_left < kStepT ? rows_left : kStepT;
-        const auto yr = step_rows(ynext, rows, yld, ywidth * (int)sizeof(YT));
-        const auto xr = step_rows(xnext, rows, xld, xwidth);
-        const auto sr = step_rows(snext, rows, sld, (xwidth + kActGroup - 1) / kActGroup);
+        yr = step_rows(ynext, rows, yld, ywidth * (int)sizeof(YT));
+        xr = step_rows(xnext, rows, xld, xwidth);
+        sr = step_rows(snext, rows, sld, (xwidth + kActGroup - 1) / kActGroup);
         if (last) {
             ynext += (int64_t)kStepT * yld;
             xnext += (int64_t)kStepT * xld;
             snext += (int64_t)kStepT * sld;
             rows_left -= kStepT;
         }
-#pragma unroll
-        for (int a = 0; a < Stage::kPassY; ++a)
-            r.y[a].load(yr, yat + (uint32_t)(a * (kStepT / Stage::kPassY)) * (uint32_t)yld);
-#pragma unroll
-        for (int a = 0; a < Stage::kPassX; ++a) {
+    };
+    constexpr int kPieces = Stage::kPassY + Stage::kPassX;
+    auto load_piece = [&](Stage& r, int piece) {
+        if (piece < Stage::kPassY) {
+            r.y[piece].load(yr, yat + (uint32_t)(piece * (kStepT / Stage::kPassY)) * (uint32_t)yld);
+        } else {
+            const int a = piece - Stage::kPassY;
             const uint32_t row = a * (kStepT / Stage::kPassX);
             r.x[a] = __builtin_amdgcn_raw_buffer_load_b64(xr, xat + row * (uint32_t)xld, 0, 0);
             r.s[a] = __builtin_amdgcn_raw_buffer_load_b8(sr, sat + row * (uint32_t)sld, 0, 0);
         }
-        if (ysplit) r.ytail = Chunk8<Y>::load1(yr, ytat);
-        if (xsplit) {
-            r.xtail = __builtin_amdgcn_raw_buffer_load_b8(xr, xtat, 0, 0);
-            r.stail = __builtin_amdgcn_raw_buffer_load_b8(sr, stat, 0, 0);
+        if (piece == kPieces - 1) {
+            if (ysplit) r.ytail = Chunk8<Y>::load1(yr, ytat);
+            if (xsplit) {
+                r.xtail = __builtin_amdgcn_raw_buffer_load_b8(xr, xtat, 0, 0);
+                r.stail = __builtin_amdgcn_raw_buffer_load_b8(sr, stat, 0, 0);
+            }
         }
+    };
+    auto load_stage = [&](Stage& r, bool last) {
+        open_stage(last);
+#pragma unroll
+        for (int a = 0; a < kPieces; ++a) load_piece(r, a);
     };
     // LDS places of what a thread stages, in the current pair of stages; a
     // change of pair flips one bit
@@ -239,24 +250,31 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     for (int a = 0; a < Stage::kPassX; ++a)
         xput[a] = kStageY + place(xrow + a * (kStepT / Stage::kPassX), xcol, kRowX);
     int ytput = place(trow, ytcol, kRowY), xtput = kStageY + place(trow, xtcol, kRowX);
-    // store into the pair that `pair` says (0 or kPair), its stage `half`
-    auto store_stage = [&](const Stage& r, auto part, int pair, int half) {
+    // store a piece into the pair that `pair` says (0 or kPair), its stage `half`
+    auto store_piece = [&](const Stage& r, auto part, int pair, int half, int piece) {
         constexpr int kPart = decltype(part)::value;
         uint8_t* to = lds + half * kStage;
-#pragma unroll
-        for (int a = 0; a < Stage::kPassY; ++a)
+        if (piece < Stage::kPassY) {
             if (!TAILS || ywhole)
-                *reinterpret_cast<u32x4*>(to + (yput[a] ^ pair)) = r.y[a].template terms<kPart>();
-#pragma unroll
-        for (int a = 0; a < Stage::kPassX; ++a)
+                *reinterpret_cast<u32x4*>(to + (yput[piece] ^ pair)) =
+                    r.y[piece].template terms<kPart>();
+        } else {
+            const int a = piece - Stage::kPassY;
             if (!TAILS || xwhole)
                 *reinterpret_cast<u32x4*>(to + (xput[a] ^ pair)) = restore8(r.x[a], r.s[a]);
-        if (ysplit)
-            *reinterpret_cast<uint16_t*>(to + (ytput ^ pair)) =
-                (uint16_t)Chunk8<Y>::template term1<kPart>(r.ytail);
-        if (xsplit)
-            *reinterpret_cast<uint16_t*>(to + (xtput ^ pair)) =
-                (uint16_t)restore8(u32x2{r.xtail, 0}, r.stail).x;
+        }
+        if (piece == kPieces - 1) {
+            if (ysplit)
+                *reinterpret_cast<uint16_t*>(to + (ytput ^ pair)) =
+                    (uint16_t)Chunk8<Y>::template term1<kPart>(r.ytail);
+            if (xsplit)
+                *reinterpret_cast<uint16_t*>(to + (xtput ^ pair)) =
+                    (uint16_t)restore8(u32x2{r.xtail, 0}, r.stail).x;
+        }
+    };
+    auto store_stage = [&](const Stage& r, auto part, int pair, int half) {
+#pragma unroll
+        for (int a = 0; a < kPieces; ++a) store_piece(r, part, pair, half, a);
     };
     auto barrier = [] {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -289,32 +307,22 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     struct Frags {
         bf16x8 y[NI], x[MI];
     };
-    auto read_frags = [&](Frags& f, int pair, int stage, int half) {
-#pragma unroll
-        for (int a = 0; a < MI; ++a) {
-            f.x[a] = fragment((xaddr[a] ^ pair) + stage * kStage + half * 16 * kRowX, kRowX);
-            if (a == 0)
-#pragma unroll
-                for (int c = 0; c < NI; ++c)
-                    f.y[c] = fragment((yaddr[c] ^ pair) + stage * kStage + half * 16 * kRowY, kRowY);
-        }
+    // fragment b in the order of their use: x 0, all y, the other x
+    constexpr int kFrags = MI + NI;
+    auto read_frag = [&](Frags& f, int pair, int stage, int half, int b) {
+        if (b >= 1 && b <= NI)
+            f.y[b - 1] = fragment((yaddr[b - 1] ^ pair) + stage * kStage + half * 16 * kRowY, kRowY);
+        else
+            f.x[b ? b - NI : 0] = fragment((xaddr[b ? b - NI : 0] ^ pair) + stage * kStage +
+                                               half * 16 * kRowX, kRowX);
     };
     f32x16 acc[MI][NI] = {};
-    auto multiply = [&](const Frags& f) {
-#pragma unroll
-        for (int a = 0; a < MI; ++a)
-#pragma unroll
-            for (int c = 0; c < NI; ++c)
-                acc[a][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.x[a], f.y[c], acc[a][c], 0,
-                                                                    0, 0);
-    };
-
     // Two steps s, s + 1 multiply one pair of stages, store tiles s + 2, s + 3 into
     // the other and load tiles s + 4, s + 5 into the registers this frees.  The
     // workgroup meets once, before the last quarter, whose fragments are then
     // read: behind it the stored pair may be read and this one stored.  A
-    // wavefront issues an instruction every 4 cycles and a product takes 32: the
-    // groups below deal the reads, stores and loads out between the products.
+    // wavefront issues an instruction every 4 cycles and a product takes 32, so
+    // reads, stores and loads are dealt out between the products.
     Stage r[2];
     Frags f0, f1;
     load_stage(r[0], kTerms == 1);
@@ -324,35 +332,36 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     store_stage(r[1], Part<1 % kTerms>(), 0, 1);
     load_stage(r[1], kTerms == 1);
     barrier();
-    read_frags(f0, 0, 0, 0);
+#pragma unroll
+    for (int b = 0; b < kFrags; ++b) read_frag(f0, 0, 0, 0, b);
     int pair = 0;
-    constexpr int kProducts = MI * NI, kReads = 2 * (MI + NI);
-    constexpr int kReadsEach = (kReads + kProducts - 1) / kProducts;
-    // step s of 2 * kTerms: term s % kTerms of token block s / kTerms
-    auto half = [&](const Frags& now, auto... after) {
-        (after(), ...);
-        multiply(now);
+    constexpr int kProducts = MI * NI;
+    // half a step: its products, and after each its share of the next half's
+    // fragments and of the pieces to be stored or loaded
+    auto half = [&](const Frags& now, auto read, auto move) {
 #pragma unroll
         for (int k = 0; k < kProducts; ++k) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);           // product
-            __builtin_amdgcn_sched_group_barrier(0x100, kReadsEach, 0);  // LDS read
-            __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);           // LDS write
-            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);           // load
+            acc[k / NI][k % NI] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                now.x[k / NI], now.y[k % NI], acc[k / NI][k % NI], 0, 0, 0);
+#pragma unroll
+            for (int b = k * kFrags / kProducts; b < (k + 1) * kFrags / kProducts; ++b) read(b);
+#pragma unroll
+            for (int a = k * kPieces / kProducts; a < (k + 1) * kPieces / kProducts; ++a) move(a);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
     };
     auto two_steps = [&](auto part) {
         constexpr int s = decltype(part)::value;
-        half(f0, [&] { read_frags(f1, pair, 0, 1); },
-             [&] { store_stage(r[0], Part<(s + 2) % kTerms>(), pair ^ kPair, 0); });
-        half(f1, [&] { read_frags(f0, pair, 1, 0); },
-             [&] { load_stage(r[0], (s + 4) % kTerms == kTerms - 1); });
-        half(f0, [&] { read_frags(f1, pair, 1, 1); },
-             [&] { store_stage(r[1], Part<(s + 3) % kTerms>(), pair ^ kPair, 1); });
+        half(f0, [&](int b) { read_frag(f1, pair, 0, 1, b); },
+             [&](int a) { store_piece(r[0], Part<(s + 2) % kTerms>(), pair ^ kPair, 0, a); });
+        open_stage((s + 4) % kTerms == kTerms - 1);
+        half(f1, [&](int b) { read_frag(f0, pair, 1, 0, b); }, [&](int a) { load_piece(r[0], a); });
+        half(f0, [&](int b) { read_frag(f1, pair, 1, 1, b); },
+             [&](int a) { store_piece(r[1], Part<(s + 3) % kTerms>(), pair ^ kPair, 1, a); });
+        open_stage((s + 5) % kTerms == kTerms - 1);
         barrier();
         pair ^= kPair;
-        half(f1, [&] { read_frags(f0, pair, 0, 0); },
-             [&] { load_stage(r[1], (s + 5) % kTerms == kTerms - 1); });
+        half(f1, [&](int b) { read_frag(f0, pair, 0, 0, b); }, [&](int a) { load_piece(r[1], a); });
     };
     for (int k = 0; k < pairs; ++k) {
         two_steps(Part<0>());
