@@ -25,11 +25,15 @@ typedef __attribute__((address_space(3))) i16x4 LdsQuad;
 constexpr int kStepT = 32;    // tokens of a step
 constexpr int kStages = 4;    // steps whose tiles are in LDS, as two pairs
 
+// The tiles of all workers in order; the first `whole` are summed by a workgroup
+// each, the other `rest` by `runs` workgroups over run_t tokens each, whose
+// fp32 sums (tile by tile, [rest][runs][edge][edge]) a second launch joins.
 struct WgradPlan {
-    int64_t tiles_o, tiles_h;
-    int splits;         // runs of tokens summed apart
-    int64_t split_t;    // tokens of a run, a multiple of kStepT
-    float* part;        // [splits][n][o][h] where splits > 1
+    int edge;
+    int64_t tiles_o, tiles_h, whole, rest;
+    int runs;
+    int64_t run_t;
+    float* part;
 };
 
 // A tile row (one token, T columns of bf16) is T / 16 units of 32 bytes; unit u
@@ -140,12 +144,49 @@ struct Part {
     static constexpr int value = N;
 };
 
+struct Tile {
+    int i;           // worker
+    int64_t o0, h0;  // corner
+};
+
+// Consecutive workgroups go to the 8 dies in turn; each die takes a contiguous
+// run of tiles.
+__device__ __forceinline__ int64_t spread(int64_t b, int64_t total) {
+    const int64_t die = b % 8, each = total / 8, more = total % 8;
+    return die * each + (die < more ? die : more) + b / 8;
+}
+
+// Tiles run through a worker's matrix in bands 4 tiles high, column by column:
+// the 32 tiles that a die works on are 4 x 8, whose dy and codes its L2 holds.
+template <int TO, int TH>
+__device__ __forceinline__ Tile tile_at(const WgradPlan& g, int64_t lin) {
+    const int64_t per = g.tiles_o * g.tiles_h;
+    const int64_t i = lin / per, tile = lin - i * per;
+    const int64_t band = tile / (4 * g.tiles_h), in = tile - band * 4 * g.tiles_h;
+    const int64_t height = g.tiles_o - band * 4 < 4 ? g.tiles_o - band * 4 : 4;
+    return Tile{(int)i, (band * 4 + in % height) * TO, in / height * TH};
+}
+
+// Row o, columns h .. h + U of a worker's gradient take U sums.
+template <class G, int U>
+__device__ __forceinline__ void put_sums(const WgradParams& p, int i, int64_t o, int64_t h,
+                                         float (&v)[U]) {
+    typedef typename G::T GT;
+    GT* d = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + o * p.h + h;
+    const int64_t have = p.h - h;
+    float old[U];
+    if (p.accumulate) load_unit<GT, U, false>(d, have, old);
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+        v[k] = p.accumulate ? __builtin_fmaf(p.scale, v[k], old[k]) : p.scale * v[k];
+    store_unit<GT, U, true>(d, have, v);
+}
+
 // A workgroup of WO x WH wavefronts owns a TO x TH tile of D over a run of
 // tokens.  TAILS: o or h is not a multiple of 8.
 template <class Y, class G, int TO, int TH, int WO, int WH, bool TAILS>
 __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan& g) {
     typedef typename Y::T YT;
-    typedef typename G::T GT;
     constexpr int kThreads = WO * WH * kWave;
     constexpr int NI = TO / WO / 32, MI = TH / WH / 32;  // 32 x 32 products of a wavefront
     constexpr int kTerms = sizeof(YT) == 4 ? 3 : 1;
@@ -155,22 +196,17 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     typedef Staged<Y, TO, TH, kThreads> Stage;
     __shared__ __attribute__((aligned(16))) uint8_t lds[kStages * kStage];
 
-    // workgroup -> (run, worker, tile): consecutive workgroups go to the 8
-    // dies in turn; each die takes a contiguous run of tiles, 4 x k blocks of
-    // them, whose rows and columns its L2 then holds
-    const int64_t per_unit = g.tiles_o * g.tiles_h;
-    const int64_t total = per_unit * p.n * g.splits;
-    const int64_t b = blockIdx.x, die = b % 8, each = total / 8, more = total % 8;
-    const int64_t lin = die * each + (die < more ? die : more) + b / 8;
-    const int64_t unit = lin / per_unit, tile = lin - unit * per_unit;
-    const int i = (int)(unit % p.n), split = (int)(unit / p.n);
-    const int64_t band = tile / (4 * g.tiles_h), in = tile - band * 4 * g.tiles_h;
-    const int64_t height = g.tiles_o - band * 4 < 4 ? g.tiles_o - band * 4 : 4;
-    const int64_t o0 = (band * 4 + in % height) * TO, h0 = in / height * TH;
-
+    const bool apart = g.runs > 1 && blockIdx.x >= g.whole;
+    const int64_t ticket = apart ? blockIdx.x - g.whole : blockIdx.x;
+    const int run = apart ? (int)(ticket % g.runs) : 0;
+    const Tile tile = tile_at<TO, TH>(
+        g, apart ? g.whole + ticket / g.runs
+                 : spread(ticket, g.runs > 1 ? g.whole : g.whole + g.rest));
+    const int i = tile.i;
+    const int64_t o0 = tile.o0, h0 = tile.h0;
     const int64_t m = batch_len(p.lengths, i, p.t);
-    const int64_t t0 = split * g.split_t;
-    const int64_t t1 = t0 + g.split_t < m ? t0 + g.split_t : m;
+    const int64_t t0 = run * g.run_t;
+    const int64_t t1 = apart && t0 + g.run_t < m ? t0 + g.run_t : m;
     // tokens in pairs of blocks; loads past the run's end give zeros
     const int left = t1 > t0 ? (int)(t1 - t0) : 0;
     const int pairs = (left + 2 * kStepT - 1) / (2 * kStepT);
@@ -371,35 +407,48 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
         }
     }
 
-    // lane -> column (output row) o, 4 x 4 consecutive h
+    // A lane holds 4 x 4 consecutive columns of one row of every 32 x 32 block.
+    // Through LDS, a wavefront's own part of it, they become whole row pieces:
+    // 32 rows at a time, padded by 16 bytes against bank conflicts.
+    constexpr int kWide = MI * 32, kPadded = kWide + 4;
+    static_assert(kWide == 64 && WO * WH * 32 * kPadded * 4 <= kStages * kStage, "LDS of the end");
+    barrier();
+    float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kPadded;
 #pragma unroll
-    for (int a = 0; a < MI; ++a)
+    for (int c = 0; c < NI; ++c) {
 #pragma unroll
-        for (int c = 0; c < NI; ++c) {
-            const int64_t o = o0 + wo + c * 32 + lane % 32;
-            if (o >= p.o) continue;
+        for (int a = 0; a < MI; ++a)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int64_t h = h0 + wh + a * 32 + e * 8 + lane / 32 * 4;
-                const int64_t have = p.h - h;
-                if (have <= 0) continue;
                 float v[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = acc[a][c][e * 4 + k];
-                if (g.splits > 1) {
-                    store_unit<float, 4, false>(
-                        g.part + (((int64_t)split * p.n + i) * p.o + o) * p.h + h, have, v);
-                    continue;
-                }
-                GT* d = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + o * p.h + h;
-                float old[4];
-                if (p.accumulate) load_unit<GT, 4, false>(d, have, old);
+                __builtin_memcpy(__builtin_assume_aligned(
+                                     mine + lane % 32 * kPadded + a * 32 + e * 8 + lane / 32 * 4, 16),
+                                 v, 16);
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (apart) {
+            float* part = g.part + ticket * TO * TH + (wo + c * 32) * TH + wh;
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    v[k] = p.accumulate ? __builtin_fmaf(p.scale, v[k], old[k]) : p.scale * v[k];
-                store_unit<GT, 4, false>(d, have, v);
+            for (int r = lane / 16; r < 32; r += 4) {
+                float v[4];
+                __builtin_memcpy(v, __builtin_assume_aligned(mine + r * kPadded + lane % 16 * 4, 16), 16);
+                store_unit<float, 4, false>(part + r * TH + lane % 16 * 4, 4, v);
+            }
+        } else {
+            constexpr int U = 16 / (int)sizeof(typename G::T), kLanes = kWide / U;
+#pragma unroll
+            for (int r = lane / kLanes; r < 32; r += kWave / kLanes) {
+                float v[U];
+                __builtin_memcpy(v, __builtin_assume_aligned(mine + r * kPadded + lane % kLanes * U, 16),
+                                 sizeof(v));
+                const int64_t o = o0 + wo + c * 32 + r, h = h0 + wh + lane % kLanes * U;
+                if (o < p.o && h < p.h) put_sums<G, U>(p, i, o, h, v);
             }
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
 }
 
 template <class Y, class G>
@@ -412,53 +461,52 @@ __global__ __launch_bounds__(256, 2) void k_act_wgrad_128(WgradParams p, WgradPl
     wgrad_tile<Y, G, 128, 128, 2, 2, true>(p, g);
 }
 
-// Sum of the runs' partial results, in order.
+// Sum of the runs of the tiles that were summed apart, in order.
+template <class G, int EDGE>
+__device__ __forceinline__ void join_tile(const WgradParams& p, const WgradPlan& g) {
+    constexpr int U = 4, kUnits = EDGE * EDGE / U, kBlocks = kUnits / kBlock;
+    const int64_t which = blockIdx.x / kBlocks;
+    const int at = (int)(blockIdx.x % kBlocks * kBlock + threadIdx.x) * U;
+    const Tile tile = tile_at<EDGE, EDGE>(g, g.whole + which);
+    const int64_t o = tile.o0 + at / EDGE, h = tile.h0 + at % EDGE;
+    if (o >= p.o || h >= p.h) return;
+    const float* part = g.part + which * g.runs * EDGE * EDGE + at;
+    float sum[U] = {};
+    for (int s = 0; s < g.runs; ++s) {
+        float v[U];
+        load_unit<float, U, false>(part + (int64_t)s * EDGE * EDGE, U, v);
+#pragma unroll
+        for (int k = 0; k < U; ++k) sum[k] += v[k];
+    }
+    put_sums<G, U>(p, tile.i, o, h, sum);
+}
+
 template <class G>
 __global__ __launch_bounds__(kBlock) void k_act_wgrad_join(WgradParams p, WgradPlan g) {
-    typedef typename G::T GT;
-    const int64_t size = p.o * p.h, units = (size + 3) / 4, total = units * p.n;
-    for (int64_t w = (int64_t)blockIdx.x * kBlock + threadIdx.x; w < total;
-         w += (int64_t)gridDim.x * kBlock) {
-        const int64_t i = w / units, c = (w - i * units) * 4, have = size - c;
-        float sum[4] = {};
-        for (int s = 0; s < g.splits; ++s) {
-            float v[4];
-            load_unit<float, 4, false>(g.part + ((int64_t)s * p.n + i) * size + c, have, v);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sum[k] += v[k];
-        }
-        GT* d = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + c;
-        float old[4];
-        if (p.accumulate) load_unit<GT, 4, false>(d, have, old);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            sum[k] = p.accumulate ? __builtin_fmaf(p.scale, sum[k], old[k]) : p.scale * sum[k];
-        store_unit<GT, 4, false>(d, have, sum);
-    }
+    if (g.edge == 256) join_tile<G, 256>(p, g);
+    else join_tile<G, 128>(p, g);
 }
 
 constexpr int kCus = 256;
 
-// Tile edge and token runs.  256 x 256 tiles where they give every compute unit
-// one (and both widths are multiples of 8), else 128 x 128; where even those are fewer than the compute units, the
-// tokens are cut into runs of at least 8 steps.
-int wgrad_plan(int64_t n, int64_t t, int64_t o, int64_t h, WgradPlan* g) {
+// Time of a plan in steps of a 256 x 256 tile
+void wgrad_plan(int64_t n, int64_t t, int64_t o, int64_t h, WgradPlan* g) {
     auto tiles = [&](int64_t e) { return n * ((o + e - 1) / e) * ((h + e - 1) / e); };
+    const int64_t steps = (t + kStepT - 1) / kStepT;
     const int edge = tiles(256) >= kCus && o % 8 == 0 && h % 8 == 0 ? 256 : 128;
+    const int64_t places = edge == 256 ? kCus : 2 * kCus;
+    g->edge = edge;
     g->tiles_o = (o + edge - 1) / edge;
     g->tiles_h = (h + edge - 1) / edge;
-    const int64_t steps = (t + kStepT - 1) / kStepT;
-    int64_t splits = 1;
-    if (tiles(edge) < kCus) {
-        splits = (2 * kCus) / tiles(edge);
-        const int64_t most = steps / 8;
-        splits = splits < most ? splits : most;
-        if (splits < 1) splits = 1;
-    }
-    const int64_t each = (steps + splits - 1) / splits;
-    g->split_t = (each < 1 ? 1 : each) * kStepT;
-    g->splits = (int)(each < 1 ? 1 : (steps + each - 1) / each);
-    return edge;
+    g->whole = tiles(edge) / places * places;
+    g->rest = tiles(edge) - g->whole;
+    int64_t runs = g->rest ? places / g->rest : 1;
+    const int64_t most = steps / 8;
+    runs = runs < most ? runs : most;
+    if (runs < 1) runs = 1;
+    const int64_t each = (steps + runs - 1) / runs;
+    g->run_t = (each < 1 ? 1 : each) * kStepT;
+    g->runs = (int)(each < 1 ? 1 : (steps + each - 1) / each);
 }
 
 }  // namespace
@@ -466,23 +514,23 @@ int wgrad_plan(int64_t n, int64_t t, int64_t o, int64_t h, WgradPlan* g) {
 size_t act_wgrad_workspace(int64_t n, int64_t t, int64_t o, int64_t h) {
     WgradPlan g;
     wgrad_plan(n, t, o, h, &g);
-    return g.splits > 1 ? (size_t)g.splits * n * o * h * 4 : 0;
+    return g.runs > 1 ? (size_t)g.rest * g.runs * g.edge * g.edge * 4 : 0;
 }
 
 hipError_t launch_act_wgrad(const WgradParams& p, void* ws, hipStream_t s) {
     WgradPlan g;
-    const int edge = wgrad_plan(p.n, p.t, p.o, p.h, &g);
+    wgrad_plan(p.n, p.t, p.o, p.h, &g);
     g.part = static_cast<float*>(ws);
-    const int64_t blocks = g.tiles_o * g.tiles_h * p.n * g.splits;
+    const int64_t blocks = g.whole + g.rest * g.runs;
     if (blocks > 0xFFFFFFFFll / 512) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks);
-    if (edge == 256)
+    if (g.edge == 256)
         LOSSY_LAUNCH2(k_act_wgrad_256, p.dy.bf16, p.grads.bf16, grid, dim3(512), s, p, g);
     else
         LOSSY_LAUNCH2(k_act_wgrad_128, p.dy.bf16, p.grads.bf16, grid, dim3(256), s, p, g);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || g.splits == 1) return e;
-    const dim3 join(grid_for((p.n * ((p.o * p.h + 3) / 4) + kBlock - 1) / kBlock));
+    if (e != hipSuccess || g.runs == 1) return e;
+    const dim3 join((unsigned)(g.rest * (g.edge * g.edge / 4 / kBlock)));
     if (p.grads.bf16)
         hipLaunchKernelGGL((k_act_wgrad_join<El16>), join, dim3(kBlock), 0, s, p, g);
     else
