@@ -29,7 +29,7 @@ constexpr int kStages = 4;    // steps whose tiles are in LDS, as two pairs
 // each, the other `rest` by `runs` workgroups over run_t tokens each, whose
 // fp32 sums (tile by tile, [rest][runs][edge][edge]) a second launch joins.
 struct WgradPlan {
-    int edge;
+    int edge;  // of the square tiles
     int64_t tiles_o, tiles_h, whole, rest;
     int runs;
     int64_t run_t;
@@ -199,9 +199,8 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     const bool apart = g.runs > 1 && blockIdx.x >= g.whole;
     const int64_t ticket = apart ? blockIdx.x - g.whole : blockIdx.x;
     const int run = apart ? (int)(ticket % g.runs) : 0;
-    const Tile tile = tile_at<TO, TH>(
-        g, apart ? g.whole + ticket / g.runs
-                 : spread(ticket, g.runs > 1 ? g.whole : g.whole + g.rest));
+    const Tile tile =
+        tile_at<TO, TH>(g, apart ? g.whole + ticket / g.runs : spread(ticket, g.whole));
     const int i = tile.i;
     const int64_t o0 = tile.o0, h0 = tile.h0;
     const int64_t m = batch_len(p.lengths, i, p.t);
@@ -472,11 +471,17 @@ __device__ __forceinline__ void join_tile(const WgradParams& p, const WgradPlan&
     if (o >= p.o || h >= p.h) return;
     const float* part = g.part + which * g.runs * EDGE * EDGE + at;
     float sum[U] = {};
-    for (int s = 0; s < g.runs; ++s) {
-        float v[U];
-        load_unit<float, U, false>(part + (int64_t)s * EDGE * EDGE, U, v);
+    constexpr int kAhead = 8;  // runs whose loads are in flight
+    for (int s = 0; s < g.runs; s += kAhead) {
+        float v[kAhead][U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) sum[k] += v[k];
+        for (int a = 0; a < kAhead; ++a)
+            if (s + a < g.runs) load_unit<float, U, true>(part + (int64_t)(s + a) * EDGE * EDGE, U, v[a]);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            if (s + a < g.runs)
+#pragma unroll
+                for (int k = 0; k < U; ++k) sum[k] += v[a][k];
     }
     put_sums<G, U>(p, tile.i, o, h, sum);
 }
@@ -487,39 +492,77 @@ __global__ __launch_bounds__(kBlock) void k_act_wgrad_join(WgradParams p, WgradP
     else join_tile<G, 128>(p, g);
 }
 
-constexpr int kCus = 256;
+// Microseconds of a plan, from measurements on square layers of 256 to 4096 and
+// 64 to 8192 tokens.  A launch with its first loads and last stores takes 9
+// (256 x 256 tiles) or 6.7 (128 x 128); a step of 32 tokens 0.57 where few
+// compute units work and 0.80 where all do, or 0.35, 0.40 and, with two tiles
+// on a compute unit, 0.55; fp32 dy takes three steps of 1.25 times that.
+// Sums kept apart cost 3 and 0.27 a megabyte.  For 2048 x 2048 and 512 tokens
+// that gives 128 x 128 tiles in one run (12.1; two runs 33.5, 256 x 256 18.8),
+// for 8192 tokens 256 x 256 in four (77.4; one run 156.4, 128 x 128 89.8).
+constexpr int64_t kCus = 256;
 
-// Time of a plan in steps of a 256 x 256 tile
-void wgrad_plan(int64_t n, int64_t t, int64_t o, int64_t h, WgradPlan* g) {
-    auto tiles = [&](int64_t e) { return n * ((o + e - 1) / e) * ((h + e - 1) / e); };
-    const int64_t steps = (t + kStepT - 1) / kStepT;
-    const int edge = tiles(256) >= kCus && o % 8 == 0 && h % 8 == 0 ? 256 : 128;
+double tiles_us(int edge, int64_t blocks, double steps) {
     const int64_t places = edge == 256 ? kCus : 2 * kCus;
-    g->edge = edge;
-    g->tiles_o = (o + edge - 1) / edge;
-    g->tiles_h = (h + edge - 1) / edge;
-    g->whole = tiles(edge) / places * places;
-    g->rest = tiles(edge) - g->whole;
-    int64_t runs = g->rest ? places / g->rest : 1;
-    const int64_t most = steps / 8;
-    runs = runs < most ? runs : most;
-    if (runs < 1) runs = 1;
-    const int64_t each = (steps + runs - 1) / runs;
-    g->run_t = (each < 1 ? 1 : each) * kStepT;
-    g->runs = (int)(each < 1 ? 1 : (steps + each - 1) / each);
+    const int64_t full = blocks / places, rest = blocks - full * places;
+    const double most = edge == 256 ? 0.80 : 0.55;
+    double last = 0.0;
+    if (rest > 0) {
+        if (edge == 256) last = 0.57 + 0.23 * rest / kCus;
+        else last = rest <= kCus ? 0.35 + 0.05 * rest / kCus : 0.55;
+    }
+    return steps * (full * most + last);
+}
+
+void wgrad_plan(int64_t n, int64_t t, int64_t o, int64_t h, bool bf16, WgradPlan* g) {
+    const int64_t steps = (t + kStepT - 1) / kStepT;
+    const double cost = bf16 ? 1.0 : 3.75;
+    double best = 0.0;
+    for (int edge = 256; edge >= 128; edge /= 2) {
+        if (edge == 256 && (o % 8 || h % 8)) continue;  // its kernel has no odd columns
+        const int64_t tiles_o = (o + edge - 1) / edge, tiles_h = (h + edge - 1) / edge;
+        const int64_t tiles = n * tiles_o * tiles_h;
+        const int64_t places = edge == 256 ? kCus : 2 * kCus;
+        for (int64_t runs = 1; runs <= 64 && (runs == 1 || runs * 2 <= steps); ++runs) {
+            const int64_t whole = runs == 1 ? tiles : tiles / places * places;
+            const int64_t rest = tiles - whole;
+            if (runs > 1 && (rest == 0 || rest * runs > 4 * kCus)) break;
+            int64_t each = (steps + runs - 1) / runs;
+            if (each < 1) each = 1;
+            double us = (edge == 256 ? 9.0 : 6.7) + tiles_us(edge, whole, cost * steps);
+            if (runs > 1)
+                us += tiles_us(edge, rest * runs, cost * each) + 3.0 +
+                      0.27e-6 * rest * runs * edge * edge * 4;
+            if (g->edge && us >= best) continue;
+            best = us;
+            g->edge = edge;
+            g->tiles_o = tiles_o;
+            g->tiles_h = tiles_h;
+            g->whole = whole;
+            g->rest = rest;
+            // as many runs as have tokens
+            g->runs = runs == 1 ? 1 : (int)((steps + each - 1) / each);
+            g->run_t = each * kStepT;
+        }
+    }
 }
 
 }  // namespace
 
 size_t act_wgrad_workspace(int64_t n, int64_t t, int64_t o, int64_t h) {
-    WgradPlan g;
-    wgrad_plan(n, t, o, h, &g);
-    return g.runs > 1 ? (size_t)g.rest * g.runs * g.edge * g.edge * 4 : 0;
+    size_t most = 0;  // of either type of dy
+    for (int bf16 = 0; bf16 < 2; ++bf16) {
+        WgradPlan g = {};
+        wgrad_plan(n, t, o, h, bf16, &g);
+        const size_t bytes = g.runs > 1 ? (size_t)g.rest * g.runs * g.edge * g.edge * 4 : 0;
+        most = bytes > most ? bytes : most;
+    }
+    return most;
 }
 
 hipError_t launch_act_wgrad(const WgradParams& p, void* ws, hipStream_t s) {
-    WgradPlan g;
-    wgrad_plan(p.n, p.t, p.o, p.h, &g);
+    WgradPlan g = {};
+    wgrad_plan(p.n, p.t, p.o, p.h, p.dy.bf16, &g);
     g.part = static_cast<float*>(ws);
     const int64_t blocks = g.whole + g.rest * g.runs;
     if (blocks > 0xFFFFFFFFll / 512) return hipErrorInvalidConfiguration;

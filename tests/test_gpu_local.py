@@ -427,7 +427,11 @@ def test_act_wgrad(n, t, o, h, ydt, gdt, offset, lens, py, pq, ps, shift, accumu
 @pytest.mark.parametrize("n,t,o,h", [(1, 4096, 256, 256), (2, 1000, 520, 264), (1, 9001, 65, 40),
                                      (3, 130, 770, 1030), (1, 700, 1025, 2049),
                                      (70, 37, 264, 520), (1, 290, 4096, 4104),
-                                     (256, 100, 40, 16)])
+                                     (256, 100, 40, 16),
+                                     # a round of whole tiles and one cut into
+                                     # runs; runs of large tiles; many runs
+                                     (1, 1024, 4096, 4352), (1, 8192, 2048, 2040),
+                                     (2, 8192, 136, 256), (1, 8001, 300, 257)])
 def test_act_wgrad_whole_numbers_are_exact(n, t, o, h, ydt, top):
     # |x| <= 3 and |dy| <= top: every partial sum is below 9001 * 3 * 500 < 2^24
     dy = ints((n, t, o), -top, top, 14, ydt)
