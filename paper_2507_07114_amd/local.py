@@ -15,7 +15,7 @@ from typing import Optional
 
 import torch
 
-from . import (LL_BF16, LL_F32, _SIGNATURES, _check, _f32, _i32, _i64, _load, _need_numel, _vp)
+from . import LL_BF16, LL_F32, _SIGNATURES, _check, _f32, _i32, _i64, _load, _need_numel, _vp
 
 __all__ = ["ll_embed", "ll_embed_grad", "ll_embed_grad_workspace_bytes", "ll_act_pack",
            "ll_act_unpack", "ll_act_wgrad", "ll_act_wgrad_workspace_bytes",
@@ -41,24 +41,35 @@ _SIGNATURES.update({
     "ll_act_wgrad_workspace_bytes": (_sz, [_i32, _i64, _i64, _i64]),
 })
 
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
 _FLOATS = {torch.float32: LL_F32, torch.bfloat16: LL_BF16}
 _INTS = {torch.int32: LL_I32, torch.int64: LL_I64}
 
 
-def _on_device(name: str, *tensors) -> torch.device:
-    """The one device that all tensors of a call are on."""
-    given = [t for t in tensors if t is not None]
-    dev = given[0].device
-    if dev.type != "cuda" or any(t.device != dev for t in given):
+def _on_device(name: str, first: torch.Tensor, *others) -> int:
+    """Index of the one GPU that all tensors of a call are on."""
+    dev = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            dev = -1
+    if dev < 0:
         raise ValueError(f"{name} needs all its tensors on one GPU, got "
-                         f"{sorted({str(t.device) for t in given})}")
+                         f"{sorted({str(t.device) for t in (first, *others) if t is not None})}")
     return dev
 
 
-def _call(name: str, dev: torch.device, *args) -> None:
-    """The C entry point on the tensors' device and its current stream."""
-    with torch.cuda.device(dev):
-        _check(name, getattr(_load(), name)(*args, torch.cuda.current_stream(dev).cuda_stream))
+def _call(name: str, dev: int, *args) -> None:
+    """The C entry point on the tensors' device and its current stream (the
+    handle alone: a small call is bound by the host)."""
+    fn = getattr(_load(), name)
+    if torch.cuda.current_device() == dev:
+        code = fn(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            code = fn(*args, _raw_stream(dev))
+    if code:
+        _check(name, code)
 
 
 def _code(t: torch.Tensor, name: str, codes: dict) -> int:
@@ -70,16 +81,17 @@ def _code(t: torch.Tensor, name: str, codes: dict) -> int:
 def _act(t: torch.Tensor, name: str, n: int, tokens: int, width: Optional[int] = None) -> int:
     """Row stride of an [n][tokens][width] tensor whose workers lie `tokens`
     rows apart."""
-    if t.dim() != 3 or t.shape[0] != n or t.shape[1] != tokens:
-        raise ValueError(f"{name} must be [{n}][{tokens}][...], got {tuple(t.shape)}")
-    if width is not None and t.shape[2] != width:
-        raise ValueError(f"{name} must have width {width}, got {t.shape[2]}")
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != n or shape[1] != tokens:
+        raise ValueError(f"{name} must be [{n}][{tokens}][...], got {tuple(shape)}")
+    if width is not None and shape[2] != width:
+        raise ValueError(f"{name} must have width {width}, got {shape[2]}")
+    if stride[2] != 1 and shape[2] > 1:
         raise ValueError(f"{name} must have unit column stride")
     # the stride of a dimension of length 1 means nothing
-    ld = t.stride(1) if tokens > 1 else (t.stride(0) if n > 1 else t.shape[2])
-    if n > 1 and tokens > 0 and t.stride(0) != tokens * ld:
-        raise ValueError(f"{name}: workers must lie {tokens} rows apart, got strides {t.stride()}")
+    ld = stride[1] if tokens > 1 else (stride[0] if n > 1 else shape[2])
+    if n > 1 and tokens > 0 and stride[0] != tokens * ld:
+        raise ValueError(f"{name}: workers must lie {tokens} rows apart, got strides {stride}")
     return ld
 
 
