@@ -9,6 +9,14 @@ namespace lossy {
 
 namespace {
 
+// Units of a lane, loaded together.  Inputs through the caches (what a layer just
+// wrote may be there), outputs past them.  8 x 4096 x 11008 bf16, us (pack /
+// unpack): 1 unit 202 / 209, 2 182 / 173, 4 181 / 181; outputs through the
+// caches, 2 units: 185 / 182.
+constexpr int kPer = 2;
+constexpr bool kStreamIn = false, kStreamOut = true;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 // Exponent k of a group's scale from the bits of its largest finite |x|:
 // 448 = 1.75 * 2^8, so a = f * 2^e (1 <= f < 2) needs k = e - 8, or e - 7
 // where f > 1.75.
@@ -37,133 +45,145 @@ __device__ __forceinline__ uint32_t group_max(uint32_t x) {
     return x;
 }
 
-// A lane takes one unit (16 bytes of x); the 4 or 8 lanes of a group agree on
-// its scale.  One pass: x read once, codes and scales written once.  All
-// lanes of a group stay in the loop together (units past the row's end carry
-// zeros), which the group's maximum needs.
+// A lane takes units of 16 bytes of x; the 4 or 8 lanes of a group agree on its
+// scale.  One pass: x read once, codes and scales written once.  Rows count
+// whole groups of lanes (units past the row's end carry zeros), so that a group's
+// lanes are always together.
 template <class X>
-__global__ __launch_bounds__(kBlock) void k_act_pack(PackParams p, int lanes) {
+__global__ __launch_bounds__(kBlock) void k_act_pack(PackParams p, FlatRows f) {
     typedef typename X::T XT;
     constexpr int U = 16 / (int)sizeof(XT), kLanes = kActGroup / U;
-    const int rows = kBlock / lanes, lane = threadIdx.x % lanes;
-    const int64_t total = (int64_t)p.n * p.t;
-    const int64_t units = (p.h + kActGroup - 1) / kActGroup * kLanes;
-    for (int64_t tk = (int64_t)blockIdx.x * rows + threadIdx.x / lanes; tk < total;
-         tk += (int64_t)gridDim.x * rows) {
-        if (!in_batch(p.lengths, (uint32_t)tk, p.t)) continue;
-        const XT* x = static_cast<const XT*>(p.x.p) + tk * p.x.ld;
-        uint8_t* q = p.c.q + tk * p.c.ld_q;
-        uint8_t* s = p.c.s + tk * p.c.ld_s;
-        for (int64_t u = lane; u < units; u += lanes) {
-            const int64_t c0 = u * U;
-            const int64_t have = p.h - c0;
-            float v[U];
-            load_unit<XT, U, true>(x + c0, have, v);
-            uint32_t top = 0, all = 0;
+    const uint32_t base = blockIdx.x * (uint32_t)(kBlock * kPer) + threadIdx.x;
+    float v[kPer][U];
+    int64_t have[kPer], tk[kPer];
+    uint32_t unit[kPer];
+#pragma unroll
+    for (int a = 0; a < kPer; ++a) {
+        const uint32_t w = base + a * kBlock;
+        const uint32_t row = flat_row(f, w);
+        unit[a] = w - row * f.units;
+        tk[a] = (int64_t)blockIdx.y * f.rows + row;
+        const bool in = row < f.rows && tk[a] < f.total && in_batch(p.lengths, (uint32_t)tk[a], p.t);
+        const int64_t c0 = (int64_t)unit[a] * U;
+        have[a] = in ? (p.h > c0 ? p.h - c0 : 0) : -1;
+        if (in)
+            load_unit<XT, U, kStreamIn>(static_cast<const XT*>(p.x.p) + tk[a] * p.x.ld + c0, have[a],
+                                   v[a]);
+    }
+#pragma unroll
+    for (int a = 0; a < kPer; ++a) {
+        if (have[a] < 0) continue;
+        uint8_t* q = p.c.q + tk[a] * p.c.ld_q + (int64_t)unit[a] * U;
+        uint32_t top = 0, all = 0;
+#pragma unroll
+        for (int c = 0; c < U; ++c) {
+            const uint32_t x = __float_as_uint(v[a][c]) & 0x7FFFFFFFu;
+            top = max(top, finite_bits(x) ? x : 0u);
+            all = max(all, x);
+        }
+        const int k = group_exp(group_max<kLanes>(top));
+        if (unit[a] % kLanes == 0)
+            p.c.s[tk[a] * p.c.ld_s + unit[a] / kLanes] = (uint8_t)(k + 127);
+        const float inv = exp2_int(-k), limit = code_limit(k);
+        uint32_t code[U / 4];
+#pragma unroll
+        for (int w = 0; w < U / 4; ++w) {
+            float z[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                z[c] = __builtin_amdgcn_fmed3f(v[a][4 * w + c] * inv, -limit, limit);
+            int r = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
+            code[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], r, true);
+        }
+        if (!finite_bits(all)) {  // rare: what is not finite becomes NaN
 #pragma unroll
             for (int c = 0; c < U; ++c) {
-                const uint32_t a = __float_as_uint(v[c]) & 0x7FFFFFFFu;
-                top = max(top, finite_bits(a) ? a : 0u);
-                all = max(all, a);
+                const uint32_t byte = 0xFFu << (8 * (c % 4));
+                if (!finite_bits(__float_as_uint(v[a][c]) & 0x7FFFFFFFu))
+                    code[c / 4] = (code[c / 4] & ~byte) | (0x7F7F7F7Fu & byte);
             }
-            const int k = group_exp(group_max<kLanes>(top));
-            if (u % kLanes == 0) s[u / kLanes] = (uint8_t)(k + 127);
-            const float inv = exp2_int(-k), limit = code_limit(k);
-            uint32_t code[U / 4];
+        }
+        if (have[a] >= U) {
+            typename RawOf<U>::T raw;
+            __builtin_memcpy(&raw, code, U);
+            store_raw<U, 1, kStreamOut>(q, raw);
+        } else {
 #pragma unroll
-            for (int w = 0; w < U / 4; ++w) {
-                float z[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    z[c] = __builtin_amdgcn_fmed3f(v[4 * w + c] * inv, -limit, limit);
-                int r = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
-                code[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], r, true);
-            }
-            if (!finite_bits(all)) {  // rare: what is not finite becomes NaN
-#pragma unroll
-                for (int c = 0; c < U; ++c) {
-                    const uint32_t byte = 0xFFu << (8 * (c % 4));
-                    if (!finite_bits(__float_as_uint(v[c]) & 0x7FFFFFFFu))
-                        code[c / 4] = (code[c / 4] & ~byte) | (0x7F7F7F7Fu & byte);
-                }
-            }
-            if (have >= U) {
-                typename RawOf<U>::T raw;
-                __builtin_memcpy(&raw, code, U);
-                store_raw<U, 1, true>(q + c0, raw);
-            } else {
-#pragma unroll
-                for (int c = 0; c < U; ++c)
-                    if (c < have) q[c0 + c] = (uint8_t)(code[c / 4] >> (8 * (c % 4)));
-            }
+            for (int c = 0; c < U; ++c)
+                if (c < have[a]) q[c] = (uint8_t)(code[c / 4] >> (8 * (c % 4)));
         }
     }
 }
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-
 template <class O>
-__global__ __launch_bounds__(kBlock) void k_act_unpack(PackParams p, int lanes) {
+__global__ __launch_bounds__(kBlock) void k_act_unpack(PackParams p, FlatRows f) {
     typedef typename O::T OT;
     constexpr int U = 16 / (int)sizeof(OT);
-    const int rows = kBlock / lanes, lane = threadIdx.x % lanes;
-    const int64_t total = (int64_t)p.n * p.t;
-    const int64_t units = (p.h + U - 1) / U;
-    for (int64_t tk = (int64_t)blockIdx.x * rows + threadIdx.x / lanes; tk < total;
-         tk += (int64_t)gridDim.x * rows) {
-        if (!in_batch(p.lengths, (uint32_t)tk, p.t)) continue;
-        OT* out = static_cast<OT*>(p.x.p) + tk * p.x.ld;
-        const uint8_t* q = p.c.q + tk * p.c.ld_q;
-        const uint8_t* s = p.c.s + tk * p.c.ld_s;
-#pragma unroll 2
-        for (int64_t u = lane; u < units; u += lanes) {
-            const int64_t c0 = u * U;
-            const int64_t have = p.h - c0;
-            uint32_t code[U / 4] = {};
-            if (have >= U) {
-                auto raw = load_raw<U, 1, true>(q + c0);
-                __builtin_memcpy(code, &raw, U);
-            } else {
+    const uint32_t base = blockIdx.x * (uint32_t)(kBlock * kPer) + threadIdx.x;
+    uint32_t code[kPer][U / 4], s[kPer];
+    int64_t have[kPer];
+    OT* out[kPer];
 #pragma unroll
-                for (int c = 0; c < U; ++c)
-                    if (c < have) code[c / 4] |= (uint32_t)q[c0 + c] << (8 * (c % 4));
-            }
-            const float scale = __uint_as_float((uint32_t)s[c0 / kActGroup] << 23);
-            float v[U];
+    for (int a = 0; a < kPer; ++a) {
+        const uint32_t w = base + a * kBlock;
+        const uint32_t row = flat_row(f, w);
+        const int64_t tk = (int64_t)blockIdx.y * f.rows + row;
+        const int64_t c0 = (int64_t)(w - row * f.units) * U;
+        const bool in = row < f.rows && tk < f.total && in_batch(p.lengths, (uint32_t)tk, p.t);
+        have[a] = in ? p.h - c0 : 0;
+        out[a] = static_cast<OT*>(p.x.p) + tk * p.x.ld + c0;
+        const uint8_t* q = p.c.q + tk * p.c.ld_q + c0;
+        if (in) s[a] = p.c.s[tk * p.c.ld_s + c0 / kActGroup];
+        if (have[a] >= U) {
+            auto raw = load_raw<U, 1, kStreamIn>(q);
+            __builtin_memcpy(code[a], &raw, U);
+        } else {
 #pragma unroll
-            for (int w = 0; w < U / 4; ++w) {
-                const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[w], false);
-                const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[w], true);
-                v[4 * w] = a.x * scale;
-                v[4 * w + 1] = a.y * scale;
-                v[4 * w + 2] = b.x * scale;
-                v[4 * w + 3] = b.y * scale;
-            }
-            store_unit<OT, U, true>(out + c0, have, v);
+            for (int b = 0; b < U / 4; ++b) code[a][b] = 0;
+#pragma unroll
+            for (int c = 0; c < U; ++c)
+                if (c < have[a]) code[a][c / 4] |= (uint32_t)q[c] << (8 * (c % 4));
         }
+    }
+#pragma unroll
+    for (int a = 0; a < kPer; ++a) {
+        if (have[a] <= 0) continue;
+        const float scale = __uint_as_float(s[a] << 23);
+        float v[U];
+#pragma unroll
+        for (int w = 0; w < U / 4; ++w) {
+            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[a][w], false);
+            const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[a][w], true);
+            v[4 * w] = lo.x * scale;
+            v[4 * w + 1] = lo.y * scale;
+            v[4 * w + 2] = hi.x * scale;
+            v[4 * w + 3] = hi.y * scale;
+        }
+        store_unit<OT, U, kStreamOut>(out[a], have[a], v);
     }
 }
 
 }  // namespace
 
 hipError_t launch_act_pack(const PackParams& p, hipStream_t s) {
-    const int64_t rows = (int64_t)p.n * p.t;
-    const int u = p.x.bf16 ? 8 : 4;
-    const int lanes = lanes_per_row(rows, (p.h + u - 1) / u);
-    const dim3 grid(grid_for((rows * lanes + kBlock - 1) / kBlock));
-    if (p.x.bf16) hipLaunchKernelGGL((k_act_pack<El16>), grid, dim3(kBlock), 0, s, p, lanes);
-    else hipLaunchKernelGGL((k_act_pack<El32>), grid, dim3(kBlock), 0, s, p, lanes);
+    const int lanes = kActGroup / (p.x.bf16 ? 8 : 4);
+    FlatRows f;
+    dim3 grid;
+    if (!flat_rows((int64_t)p.n * p.t, (p.h + kActGroup - 1) / kActGroup * lanes, kPer, &f, &grid))
+        return hipErrorInvalidConfiguration;
+    if (p.x.bf16) hipLaunchKernelGGL((k_act_pack<El16>), grid, dim3(kBlock), 0, s, p, f);
+    else hipLaunchKernelGGL((k_act_pack<El32>), grid, dim3(kBlock), 0, s, p, f);
     return hipGetLastError();
 }
 
 hipError_t launch_act_unpack(const PackParams& p, hipStream_t s) {
-    const int64_t rows = (int64_t)p.n * p.t;
     const int u = p.x.bf16 ? 8 : 4;
-    const int lanes = lanes_per_row(rows, (p.h + u - 1) / u);
-    const dim3 grid(grid_for((rows * lanes + kBlock - 1) / kBlock));
-    if (p.x.bf16) hipLaunchKernelGGL((k_act_unpack<El16>), grid, dim3(kBlock), 0, s, p, lanes);
-    else hipLaunchKernelGGL((k_act_unpack<El32>), grid, dim3(kBlock), 0, s, p, lanes);
+    FlatRows f;
+    dim3 grid;
+    if (!flat_rows((int64_t)p.n * p.t, (p.h + u - 1) / u, kPer, &f, &grid))
+        return hipErrorInvalidConfiguration;
+    if (p.x.bf16) hipLaunchKernelGGL((k_act_unpack<El16>), grid, dim3(kBlock), 0, s, p, f);
+    else hipLaunchKernelGGL((k_act_unpack<El32>), grid, dim3(kBlock), 0, s, p, f);
     return hipGetLastError();
 }
 

@@ -163,15 +163,50 @@ inline unsigned grid_for(int64_t blocks) {
     return (unsigned)(blocks < 1 ? 1 : (blocks > cap ? cap : blocks));
 }
 
-// Threads along a row's units (a power of two from 8 to kBlock) when a
-// workgroup takes kBlock / lanes rows: as many as a short row has units; a
-// whole wavefront per row where the rows alone fill the chip (each lane then has
-// several accesses in flight), the whole workgroup where they do not.
-inline int lanes_per_row(int64_t rows, int64_t units) {
-    const int most = rows >= 4096 ? kWave : kBlock;
+// Lanes that walk a row of that many units: a power of two from 8 to 128.
+inline int lanes_per_row(int64_t units) {
     int lanes = 8;
-    while (lanes < most && lanes < units) lanes *= 2;
+    while (lanes < kBlock / 2 && lanes < units) lanes *= 2;
     return lanes;
+}
+
+// Units of token rows, dealt out flat: a workgroup takes kBlock * PER consecutive
+// units of a group of rows, whatever rows they belong to, so that the chip
+// as a whole works on one stretch of memory (a wavefront walking a row of its
+// own reads 4.8 TB/s where this reads 6).  Rows are grouped so that a unit's
+// number inside the group has 31 bits; grid.x runs through a group, grid.y over
+// the groups.
+struct FlatRows {
+    uint32_t units, rows;  // units of a row, rows of a group
+    uint32_t mul, shift;   // unit / units = unit * mul >> shift
+    int64_t total;         // rows of all groups
+};
+
+__device__ __forceinline__ uint32_t flat_row(const FlatRows& f, uint32_t unit) {
+    return (uint32_t)(((uint64_t)unit * f.mul) >> f.shift);
+}
+
+// With s = ceil(log2 units) and mul = ceil(2^(31 + s) / units) the quotient is
+// exact for 31-bit numbers: the excess mul * units - 2^(31 + s) is below 2^s.
+// Returns the grid; false where the rows are too many for one.
+inline bool flat_rows(int64_t total, int64_t units, int per, FlatRows* f, dim3* grid) {
+    int s = 0;
+    while ((1ll << s) < units) ++s;
+    f->units = (uint32_t)units;
+    f->mul = (uint32_t)(((1ull << (31 + s)) + units - 1) / units);
+    f->shift = 31 + s;
+    f->total = total;
+    const int64_t span = kBlock * (int64_t)per;
+    int64_t rows = (0x7FFFFFFFll - span) / units;
+    rows = rows < total ? rows : total;
+    // 2^23 workgroups of 256 threads stay below 2^32 threads
+    if (rows * units > span << 23) rows = (span << 23) / units;
+    if (rows < 1) return false;
+    f->rows = (uint32_t)rows;
+    const int64_t y = (total + rows - 1) / rows;
+    if (y > 65535) return false;
+    *grid = dim3((unsigned)((rows * units + span - 1) / span), (unsigned)y);
+    return true;
 }
 
 }  // namespace lossy
