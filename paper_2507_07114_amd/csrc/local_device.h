@@ -133,15 +133,19 @@ __device__ __forceinline__ bool in_batch(const int32_t* lengths, uint32_t tk, in
     return (int64_t)(tk - i * (uint32_t)t) < lengths[i];
 }
 
-// Table row of token j of worker i, or -1 where the table does not hold it.
-__device__ __forceinline__ int64_t table_row(const TokenView& tok, int i, int64_t j) {
-    const int64_t at = (int64_t)i * tok.ld + j;
-    const int64_t id = tok.wide ? static_cast<const int64_t*>(tok.ids)[at]
-                                : (int64_t) static_cast<const int32_t*>(tok.ids)[at];
-    // held ids are first .. first + v - 1; the unsigned difference wraps where
-    // id < first, and where id - first would overflow
+// Table row of a token, or -1 where the table does not hold it.  Held ids are
+// first .. first + v - 1; the unsigned difference wraps where id < first, and
+// where id - first would overflow.
+__device__ __forceinline__ int64_t table_row(const TokenView& tok, int64_t id) {
     const uint64_t row = (uint64_t)id - (uint64_t)tok.first;
     return row < (uint64_t)tok.v ? (int64_t)row : -1;
+}
+
+// The same of token j of worker i.
+__device__ __forceinline__ int64_t table_row(const TokenView& tok, int i, int64_t j) {
+    const int64_t at = (int64_t)i * tok.ld + j;
+    return table_row(tok, tok.wide ? static_cast<const int64_t*>(tok.ids)[at]
+                                   : (int64_t) static_cast<const int32_t*>(tok.ids)[at]);
 }
 
 // Launch K<A, B> for the element types given as truth values (bf16?).

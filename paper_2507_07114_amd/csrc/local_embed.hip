@@ -73,44 +73,83 @@ constexpr int kMinSlices = 64;
 struct Sorted {
     int32_t* row;    // [n][t] table rows, grouped
     int32_t* place;  // [n][t] token places, ascending inside a row
-    int32_t* count;  // [n][v] tokens of each table row
+    int32_t* count;  // [n][slices][bins] tokens of each table row, slice by slice
     int32_t* held;   // [n] sorted tokens of a worker
     int log_slices;
+    int64_t bins;  // most rows of a slice
+
+    // Where row r of worker i is counted.  Slices lie apart: their workgroups
+    // run on several dies, whose caches would share every line of counts in
+    // the order of the rows.
+    __device__ __forceinline__ int64_t at(int i, int64_t r) const {
+        const int64_t slice = r & ((1 << log_slices) - 1);
+        return ((((int64_t)i << log_slices) + slice) * bins) + (r >> log_slices);
+    }
 };
 
 struct GradPlan {
     Sorted s;
     float* part;    // [n][chunks][2][h] partial sums
     int chunk;      // sorted tokens of a wavefront
-    int64_t chunks, strips;
-    int64_t chunk_waves, zero_waves;
+    int64_t chunks, strips, chunk_blocks;
+    int zero_rows;        // table rows of a workgroup that stores zeros, at most 64
+    int64_t zero_blocks;  // such workgroups of a worker
+    FlatRows units;       // 16-byte units of a table row
 };
-
-constexpr int kZeroRows = 4;  // table rows of a wavefront that stores zeros
 
 __global__ __launch_bounds__(kSortThreads) void k_token_sort(int64_t t, const int32_t* lengths,
                                                             TokenView tok, Sorted o) {
     __shared__ int hist[kSortWaves][kMaxBins];
     __shared__ int wave_less[kSortWaves], wave_sum[kMaxBins / kWave];
     const int slices = 1 << o.log_slices;
-    const int i = (int)(blockIdx.x >> o.log_slices), slice = (int)(blockIdx.x & (slices - 1));
-    const int w = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int i = (int)(blockIdx.x >> o.log_slices);
+    const uint32_t slice = blockIdx.x & (slices - 1);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int64_t m = batch_len(lengths, i, t);
     // rows slice, slice + slices, ... below v
-    const int bins = slice < tok.v ? (int)((tok.v - 1 - slice) >> o.log_slices) + 1 : 0;
+    const int bins = slice < tok.v ? (int)((tok.v - 1 - (int64_t)slice) >> o.log_slices) + 1 : 0;
     for (int b = threadIdx.x; b < kSortWaves * kMaxBins; b += kSortThreads)
         (&hist[0][0])[b] = 0;
     __syncthreads();
 
-    // each wavefront owns a run of places, 64 at a time
+    // each wavefront owns a run of places; kAhead tokens of a lane are loaded
+    // together (and again in the second pass: the cache has them)
+    constexpr int kAhead = 8;
     const int64_t run = (m + kSortThreads - 1) / kSortThreads * kWave;
     const int64_t j0 = w * run, j1 = j0 + run < m ? j0 + run : m;
+    uint32_t row[kAhead];
+    auto load = [&](int64_t j) {  // all loads before the first use
+        int64_t id[kAhead];
+        const int64_t first = (int64_t)i * tok.ld, last = j1 - 1;
+        if (tok.wide) {
+            const int64_t* ids = static_cast<const int64_t*>(tok.ids) + first;
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const int64_t at = j + a * kWave + lane;
+                id[a] = ids[at < last ? at : last];
+            }
+        } else {
+            const int32_t* ids = static_cast<const int32_t*>(tok.ids) + first;
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const int64_t at = j + a * kWave + lane;
+                id[a] = ids[at < last ? at : last];
+            }
+        }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            row[a] = j + a * kWave + lane < j1 ? (uint32_t)table_row(tok, id[a]) : ~0u;
+    };
+    // the slice of a row that is held; more than any where it is not
+    const uint32_t low = (slices - 1) | 0x80000000u;
     int less = 0;
-    for (int64_t j = j0; j < j1; j += kWave) {
-        const int64_t row = j + lane < j1 ? table_row(tok, i, j + lane) : -1;
-        const int at = (int)(row & (slices - 1));
-        less += __popcll(__ballot(row >= 0 && at < slice));
-        if (row >= 0 && at == slice) atomicAdd(&hist[w][row >> o.log_slices], 1);
+    for (int64_t j = j0; j < j1; j += kAhead * kWave) {
+        load(j);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            less += __popcll(__ballot((row[a] & low) < slice));
+            if ((row[a] & low) == slice) atomicAdd(&hist[w][row[a] >> o.log_slices], 1);
+        }
     }
     if (lane == 0) wave_less[w] = less;
     __syncthreads();
@@ -134,39 +173,42 @@ __global__ __launch_bounds__(kSortThreads) void k_token_sort(int64_t t, const in
         for (int a = 0; a < w; ++a) base += wave_sum[a];
         base += upto - total;
         if ((int)threadIdx.x < bins)
-            o.count[(int64_t)i * tok.v + ((int64_t)threadIdx.x << o.log_slices) + slice] = total;
+            o.count[o.at(i, slice) + threadIdx.x] = total;
         int next = base;
         for (int a = 0; a < kSortWaves; ++a) {
             const int x = hist[a][threadIdx.x];
             hist[a][threadIdx.x] = next;
             next += x;
         }
-        if (slice == slices - 1 && threadIdx.x == kMaxBins - 1) o.held[i] = next;
+        if ((int)slice == slices - 1 && threadIdx.x == kMaxBins - 1) o.held[i] = next;
     }
     __syncthreads();
     if (own == 0) return;
 
-    for (int64_t j = j0; j < j1; j += kWave) {
-        const int64_t row = j + lane < j1 ? table_row(tok, i, j + lane) : -1;
-        const bool mine = row >= 0 && (int)(row & (slices - 1)) == slice;
-        const int bin = mine ? (int)(row >> o.log_slices) : -1;
-        uint64_t left = __ballot(mine);
-        while (left) {  // a turn for each different row among the 64 tokens
-            const int lead = __ffsll((unsigned long long)left) - 1;
-            const int b = __builtin_amdgcn_readlane(bin, lead);
-            const uint64_t peers = __ballot(bin == b);
-            const int first = hist[w][b];
-            if (bin == b) {
-                const int at = first + __popcll(peers & ((1ull << lane) - 1));
-                o.row[i * t + at] = (int32_t)row;
-                o.place[i * t + at] = (int32_t)(j + lane);
+    for (int64_t j = j0; j < j1; j += kAhead * kWave) {
+        if (run > kAhead * kWave) load(j);  // else the registers still hold them
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const bool mine = (row[a] & low) == slice;
+            const int bin = mine ? (int)(row[a] >> o.log_slices) : -1;
+            uint64_t left = __ballot(mine);
+            while (left) {  // a turn for each different row among the 64 tokens
+                const int lead = __ffsll((unsigned long long)left) - 1;
+                const int b = __builtin_amdgcn_readlane(bin, lead);
+                const uint64_t peers = __ballot(bin == b);
+                const int first = hist[w][b];
+                if (bin == b) {
+                    const int at = first + __popcll(peers & ((1ull << lane) - 1));
+                    o.row[i * t + at] = (int32_t)row[a];
+                    o.place[i * t + at] = (int32_t)(j + a * kWave + lane);
+                }
+                // the wavefront's own counts: no other touches them, and its
+                // LDS accesses complete in order, so the compiler's order is
+                // all that has to be fixed
+                if (lane == lead) hist[w][b] = first + __popcll(peers);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                left &= ~peers;
             }
-            // the wavefront's own counts: no other touches them, and its LDS
-            // accesses complete in order, so the compiler's order is all that
-            // has to be fixed
-            if (lane == lead) hist[w][b] = first + __popcll(peers);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            left &= ~peers;
         }
     }
 }
@@ -179,16 +221,19 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradParams& p, const GradPl
     typedef typename Y::T YT;
     typedef typename G::T GT;
     constexpr int U = 16 / (int)sizeof(YT);
-    constexpr int kAhead = 8;  // tokens whose loads are in flight
+    constexpr int kAhead = 4;  // tokens whose loads are in flight
+    // all of these loads at once; what lies behind the held tokens is not used
+    const int32_t* rows = g.s.row + i * p.t;
+    const int64_t k0 = chunk * g.chunk, k1 = k0 + g.chunk, last = p.t - 1;
+    const int64_t mine = k0 + lane < last ? k0 + lane : last;
     const int held = g.s.held[i];
-    const int64_t k0 = chunk * g.chunk;
+    int my_row = rows[mine];
+    const int my_place = g.s.place[i * p.t + mine];
+    int before = rows[k0 > 0 ? k0 - 1 : 0], after = rows[k1 < last ? k1 : last];
     if (k0 >= held) return;
     const int len = (int)(held - k0 < g.chunk ? held - k0 : g.chunk);
-    const int32_t* rows = g.s.row + i * p.t;
-    const int my_row = lane < len ? rows[k0 + lane] : -1;
-    const int my_place = lane < len ? g.s.place[i * p.t + k0 + lane] : 0;
-    const int before = k0 > 0 ? rows[k0 - 1] : -1;
-    const int after = k0 + len < held ? rows[k0 + len] : -1;
+    before = k0 > 0 ? before : -1;
+    after = k1 < held ? after : -1;
     const int64_t c0 = (strip * kWave + lane) * U;
     const int64_t have = p.h - c0;
     const YT* dy = static_cast<const YT*>(p.dy.p) + i * p.t * p.dy.ld + c0;
@@ -235,36 +280,42 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradParams& p, const GradPl
     }
 }
 
+// A workgroup's rows that no token names: 8 KiB, or a row, 4 KiB at a time (8
+// workers' 25,695 rows of 4096 bf16 columns, no tokens: 300 us; 16 KiB 322, 64
+// KiB 345).  The counts come first, one to a lane, so that nothing stands between
+// the stores.
 template <class G>
-__device__ __forceinline__ void zero_rows(const EmbedGradParams& p, const GradPlan& g, int64_t w,
-                                          int lane) {
+__device__ __forceinline__ void zero_rows(const EmbedGradParams& p, const GradPlan& g, int64_t b) {
     typedef typename G::T GT;
     constexpr int U = 16 / (int)sizeof(GT);
-    const int64_t v = p.tok.v, groups = (v + kZeroRows - 1) / kZeroRows;
-    const int i = (int)(w / groups);
-    const int64_t r0 = (w - i * groups) * kZeroRows;
-    const int64_t r1 = r0 + kZeroRows < v ? r0 + kZeroRows : v;
-    GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset;
+    const int i = (int)(b / g.zero_blocks);
+    const int64_t r0 = (b - i * g.zero_blocks) * g.zero_rows;
+    const int rows = (int)(p.tok.v - r0 < g.zero_rows ? p.tok.v - r0 : g.zero_rows);
+    const int lane = threadIdx.x % kWave;
+    const uint64_t empty = __ballot(lane < rows && g.s.count[g.s.at(i, r0 + lane)] == 0);
+    GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + r0 * p.h;
+    const uint32_t units = rows * g.units.units;
     const float zero[U] = {};
-    for (int64_t r = r0; r < r1; ++r) {
-        if (g.s.count[i * v + r]) continue;
-        for (int64_t c = lane * U; c < p.h; c += kWave * U)
-            store_unit<GT, U, true>(grads + r * p.h + c, p.h - c, zero);
+    for (uint32_t u = threadIdx.x; u < units; u += kBlock) {
+        const uint32_t r = flat_row(g.units, u);
+        if (!(empty >> r & 1)) continue;
+        const int64_t c0 = (int64_t)(u - r * g.units.units) * U;
+        store_unit<GT, U, true>(grads + r * p.h + c0, p.h - c0, zero);
     }
 }
 
 template <class Y, class G>
-__global__ __launch_bounds__(kBlock) void k_embed_grad(EmbedGradParams p, GradPlan g) {
-    const int64_t w = (int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave;
-    const int lane = threadIdx.x % kWave;
-    if (w < g.chunk_waves) {
-        const int64_t per = g.chunks * g.strips;
-        const int i = (int)(w / per);
-        const int64_t c = (w - i * per) / g.strips;
-        sum_chunk<Y, G>(p, g, i, c, w - i * per - c * g.strips, lane);
-    } else if (w - g.chunk_waves < g.zero_waves) {
-        zero_rows<G>(p, g, w - g.chunk_waves, lane);
+__global__ __launch_bounds__(kBlock, 8) void k_embed_grad(EmbedGradParams p, GradPlan g) {
+    if (blockIdx.x >= g.chunk_blocks) {
+        zero_rows<G>(p, g, blockIdx.x - g.chunk_blocks);
+        return;
     }
+    const int64_t w = (int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave;
+    const int64_t per = g.chunks * g.strips;
+    if (w >= p.n * per) return;
+    const int i = (int)(w / per);
+    const int64_t c = (w - i * per) / g.strips;
+    sum_chunk<Y, G>(p, g, i, c, w - i * per - c * g.strips, threadIdx.x % kWave);
 }
 
 // Step 3: the wavefront of the chunk in which a crossing row begins adds the
@@ -279,27 +330,37 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, G
     if (w >= p.n * per) return;
     const int i = (int)(w / per);
     const int64_t chunk = (w - i * per) / strips, strip = w - i * per - chunk * strips;
-    const int64_t c0 = (strip * kWave + threadIdx.x % kWave) * U;
+    const int lane = threadIdx.x % kWave;
+    const int64_t c0 = (strip * kWave + lane) * U;
     const int64_t have = p.h - c0;
-    const int held = g.s.held[i];
     const int32_t* rows = g.s.row + i * p.t;
-    const int64_t k0 = chunk * g.chunk, k1 = k0 + g.chunk;
-    if (k1 >= held || have <= 0) return;
-    const int row = rows[k1 - 1];
-    if (rows[k1] != row) return;                  // does not cross
-    if (k0 > 0 && rows[k0 - 1] == row) return;  // began earlier
+    const int64_t k0 = chunk * g.chunk, k1 = k0 + g.chunk, last = p.t - 1;
+    const int held = g.s.held[i];
+    const int mine = rows[k0 + lane < last ? k0 + lane : last];
+    const int before = rows[k0 > 0 ? k0 - 1 : 0], after = rows[k1 < last ? k1 : last];
+    const int row = __builtin_amdgcn_readlane(mine, g.chunk - 1);
+    if (k1 >= held || after != row) return;  // does not cross
+    if (k0 > 0 && before == row) return;     // began earlier
+    // the further chunks that hold the rest of its tokens
+    const int here = __popcll(__ballot(lane < g.chunk && mine == row));
+    const int more = (g.s.count[g.s.at(i, row)] - here + g.chunk - 1) / g.chunk;
     const float* part = g.part + (i * g.chunks + chunk) * 2 * p.h + c0;
     float sum[U];
     load_unit<float, U, false>(part + p.h, have, sum);
-    int64_t c = chunk + 1;
-    for (;; ++c) {
-        float x[U];
-        load_unit<float, U, false>(part + (c - chunk) * 2 * p.h, have, x);
+    constexpr int kAhead = 8;  // partial sums whose loads are in flight
+    for (int a0 = 1; a0 <= more; a0 += kAhead) {
+        float x[kAhead][U];
 #pragma unroll
-        for (int a = 0; a < U; ++a) sum[a] += x[a];
-        const int64_t end = (c + 1) * g.chunk;
-        if (end >= held || rows[end] != row) break;
+        for (int a = 0; a < kAhead; ++a)
+            if (a0 + a <= more)
+                load_unit<float, U, false>(part + (int64_t)(a0 + a) * 2 * p.h, have, x[a]);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            if (a0 + a <= more)
+#pragma unroll
+                for (int k = 0; k < U; ++k) sum[k] += x[a][k];
     }
+    if (have <= 0) return;
     GT* d = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + (int64_t)row * p.h + c0;
     float out[U];
     if (p.accumulate) load_unit<GT, U, false>(d, have, out);
@@ -325,6 +386,7 @@ size_t grad_plan(int64_t n, int64_t t, int64_t h, int64_t v, uint8_t* ws, GradPl
     while ((1ll << g->s.log_slices) < kMinSlices ||
            (v - 1) >> g->s.log_slices >= kMaxBins)
         ++g->s.log_slices;
+    g->s.bins = ((v - 1) >> g->s.log_slices) + 1;
     g->chunk = chunk_of(n, t, h);
     g->chunks = (t + g->chunk - 1) / g->chunk;
     size_t at = 0;
@@ -335,7 +397,7 @@ size_t grad_plan(int64_t n, int64_t t, int64_t h, int64_t v, uint8_t* ws, GradPl
     };
     g->s.row = reinterpret_cast<int32_t*>(take((size_t)n * t * 4));
     g->s.place = reinterpret_cast<int32_t*>(take((size_t)n * t * 4));
-    g->s.count = reinterpret_cast<int32_t*>(take((size_t)n * v * 4));
+    g->s.count = reinterpret_cast<int32_t*>(take(((size_t)n << g->s.log_slices) * g->s.bins * 4));
     g->s.held = reinterpret_cast<int32_t*>(take((size_t)n * 4));
     g->part = reinterpret_cast<float*>(take((size_t)n * g->chunks * 2 * h * 4));
     return at;
@@ -362,10 +424,18 @@ hipError_t launch_embed_grad(const EmbedGradParams& p, void* ws, hipStream_t s) 
     grad_plan(p.n, p.t, p.h, p.tok.v, static_cast<uint8_t*>(ws), &g);
     const int u = p.dy.bf16 ? 8 : 4;
     g.strips = (p.h + kWave * u - 1) / (kWave * u);
-    g.chunk_waves = p.n * g.chunks * g.strips;
-    g.zero_waves = p.accumulate ? 0 : p.n * ((p.tok.v + kZeroRows - 1) / kZeroRows);
+    g.chunk_blocks = (p.n * g.chunks * g.strips + 3) / 4;
+    int64_t blocks = g.chunk_blocks;
+    if (!p.accumulate) {
+        const int64_t units = (p.h + (p.grads.bf16 ? 7 : 3)) / (p.grads.bf16 ? 8 : 4);
+        const int64_t rows = 512 / units;
+        g.zero_rows = (int)(rows < 1 ? 1 : (rows > kWave ? kWave : rows));
+        g.zero_blocks = (p.tok.v + g.zero_rows - 1) / g.zero_rows;
+        dim3 unused;
+        if (!flat_rows(g.zero_rows, units, 1, &g.units, &unused)) return hipErrorInvalidConfiguration;
+        blocks += p.n * g.zero_blocks;
+    }
     const int64_t sorts = (int64_t)p.n << g.s.log_slices;
-    const int64_t blocks = (g.chunk_waves + g.zero_waves + 3) / 4;
     const int64_t joins = (p.n * g.chunks * ((p.h + 255) / 256) + 3) / 4;
     // threads of a launch fit 32 bits
     if (sorts > 0xFFFFFFFFll / kSortThreads || blocks > 0xFFFFFFFFll / kBlock ||
