@@ -141,11 +141,15 @@ __device__ __forceinline__ int64_t table_row(const TokenView& tok, int64_t id) {
     return row < (uint64_t)tok.v ? (int64_t)row : -1;
 }
 
-// The same of token j of worker i.
-__device__ __forceinline__ int64_t table_row(const TokenView& tok, int i, int64_t j) {
+// Token j of worker i.
+__device__ __forceinline__ int64_t token_id(const TokenView& tok, int i, int64_t j) {
     const int64_t at = (int64_t)i * tok.ld + j;
-    return table_row(tok, tok.wide ? static_cast<const int64_t*>(tok.ids)[at]
-                                   : (int64_t) static_cast<const int32_t*>(tok.ids)[at]);
+    return tok.wide ? static_cast<const int64_t*>(tok.ids)[at]
+                    : (int64_t) static_cast<const int32_t*>(tok.ids)[at];
+}
+
+__device__ __forceinline__ int64_t table_row(const TokenView& tok, int i, int64_t j) {
+    return table_row(tok, token_id(tok, i, j));
 }
 
 // Launch K<A, B> for the element types given as truth values (bf16?).

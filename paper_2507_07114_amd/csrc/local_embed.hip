@@ -213,6 +213,19 @@ __global__ __launch_bounds__(kSortThreads) void k_token_sort(int64_t t, const in
     }
 }
 
+// Up to so many tokens a worker the gradient takes one launch, without sorting.
+// us against the three launches: 8 workers' 256 tokens of 25,695 x 4096 bf16
+// 261 / 299, one worker's 256 of 32000 x 4096 45 / 56, 200 of 1000 x 2048 9 / 16, 256
+// of 50 x 512 (4 workers) 13 / 16; 500 of 60000 x 128 (2 workers) 60 / 23.
+constexpr int kFewTokens = 256;
+constexpr uint32_t kFewUnits = 512;  // units of a workgroup
+
+struct FewPlan {
+    int rows;                // table rows of a workgroup, at most 64
+    int64_t groups, spans;   // such groups of a worker, workgroups of a group
+    FlatRows units;          // units of a table row
+};
+
 // One wavefront of step 2.  U columns a lane; rows and places of the chunk lie
 // one to a lane.
 template <class Y, class G>
@@ -370,6 +383,109 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, G
     store_unit<GT, U, true>(d, have, out);
 }
 
+// Few tokens: one launch, without sorting.  A workgroup takes table rows of about
+// 8 KiB (or a piece of a wide row), looks all the worker's tokens through, keeps
+// those of its rows in order, and each lane adds up its unit's.
+template <class Y, class G>
+__global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, FewPlan g) {
+    typedef typename Y::T YT;
+    typedef typename G::T GT;
+    constexpr int U = unit_of<Y, G>();
+    constexpr int kWaves = kBlock / kWave, kEach = kFewTokens / kBlock;
+    constexpr int kAhead = 4;  // tokens whose loads are in flight
+    __shared__ uint16_t place[kFewTokens];
+    __shared__ uint8_t owner[kFewTokens];
+    __shared__ int found[kWaves];
+    const int64_t span = blockIdx.x % g.spans, group = blockIdx.x / g.spans;
+    const int i = (int)(group / g.groups);
+    const int64_t r0 = (group - i * g.groups) * g.rows;
+    const int rows = (int)(p.tok.v - r0 < g.rows ? p.tok.v - r0 : g.rows);
+    const int m = (int)batch_len(p.lengths, i, p.t);
+    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
+
+    // a wavefront looks kEach * 64 consecutive tokens through
+    const int j0 = w * kEach * kWave + lane;
+    int row[kEach], mine = 0;
+    uint64_t hits[kEach];
+    int64_t id[kEach];
+#pragma unroll
+    for (int a = 0; a < kEach; ++a) {
+        const int j = j0 + a * kWave;
+        id[a] = m > 0 ? token_id(p.tok, i, j < m ? j : m - 1) : 0;
+    }
+#pragma unroll
+    for (int a = 0; a < kEach; ++a) {
+        const int64_t at = j0 + a * kWave < m ? table_row(p.tok, id[a]) - r0 : -1;
+        row[a] = at >= 0 && at < rows ? (int)at : -1;
+        hits[a] = __ballot(row[a] >= 0);
+        mine += __popcll(hits[a]);
+    }
+    if (lane == 0) found[w] = mine;
+    __syncthreads();
+    int at = 0, total = 0;
+#pragma unroll
+    for (int a = 0; a < kWaves; ++a) {
+        at += a < w ? found[a] : 0;
+        total += found[a];
+    }
+#pragma unroll
+    for (int a = 0; a < kEach; ++a) {
+        if (row[a] >= 0) {
+            const int k = at + __popcll(hits[a] & ((1ull << lane) - 1));
+            place[k] = (uint16_t)(j0 + a * kWave);
+            owner[k] = (uint8_t)row[a];
+        }
+        at += __popcll(hits[a]);
+    }
+    __syncthreads();
+    if (total == 0 && p.accumulate) return;
+
+    const YT* dy = static_cast<const YT*>(p.dy.p) + (int64_t)i * p.t * p.dy.ld;
+    GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + r0 * p.h;
+    const uint32_t all = rows * g.units.units;
+    const uint32_t u0 = (uint32_t)span * kFewUnits;
+    const uint32_t u1 = all - u0 < kFewUnits ? all : u0 + kFewUnits;
+    for (uint32_t u = u0 + threadIdx.x; u < u1; u += kBlock) {
+        const int r = (int)flat_row(g.units, u);
+        const int64_t c0 = (int64_t)(u - r * g.units.units) * U, have = p.h - c0;
+        float sum[U] = {};
+        bool any = false;
+        for (int k = 0; k < total;) {
+            int at[kAhead], n = 0;
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                while (k < total && owner[k] != r) ++k;
+                at[a] = k < total ? place[k] : -1;
+                n += k < total;
+                ++k;
+            }
+            float y[kAhead][U];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a)
+                if (a < n) load_unit<YT, U, false>(dy + at[a] * p.dy.ld + c0, have, y[a]);
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a)
+                if (a < n)
+#pragma unroll
+                    for (int c = 0; c < U; ++c) sum[c] += y[a][c];
+            any |= n > 0;
+        }
+        GT* d = grads + r * p.h + c0;
+        if (p.accumulate) {
+            if (!any) continue;
+            float old[U];
+            load_unit<GT, U, false>(d, have, old);
+#pragma unroll
+            for (int c = 0; c < U; ++c) sum[c] = __builtin_fmaf(p.scale, sum[c], old[c]);
+        } else {
+            // an empty row is 0, not -0
+#pragma unroll
+            for (int c = 0; c < U; ++c) sum[c] = any ? p.scale * sum[c] : 0.0f;
+        }
+        store_unit<GT, U, true>(d, have, sum);
+    }
+}
+
 size_t round16(size_t x) { return (x + 15) & ~(size_t)15; }
 
 // Sorted tokens of a wavefront: 64, fewer where that leaves fewer than 2048
@@ -415,11 +531,32 @@ hipError_t launch_embed(const EmbedParams& p, hipStream_t s) {
 }
 
 size_t embed_grad_workspace(int64_t n, int64_t t, int64_t h, int64_t v) {
+    if (t <= kFewTokens) return 0;
     GradPlan g;
     return grad_plan(n, t, h, v, nullptr, &g);
 }
 
+static hipError_t launch_embed_grad_few(const EmbedGradParams& p, hipStream_t s) {
+    FewPlan g;
+    const int64_t units = (p.h + 7) / 8, wide = (p.h + 3) / 4;
+    const int64_t row = p.dy.bf16 || p.grads.bf16 ? units : wide;
+    const int64_t rows = kFewUnits / row;
+    // fewer where that leaves fewer workgroups than two to a compute unit
+    const int64_t few = p.n * p.tok.v / 512, most = rows < few ? rows : few;
+    g.rows = (int)(most < 1 ? 1 : (most > kWave ? kWave : most));
+    g.groups = (p.tok.v + g.rows - 1) / g.rows;
+    g.spans = (g.rows * row + kFewUnits - 1) / kFewUnits;
+    dim3 unused;
+    const int64_t blocks = p.n * g.groups * g.spans;
+    if (!flat_rows(g.rows, row, 1, &g.units, &unused) || blocks > 0xFFFFFFFFll / kBlock)
+        return hipErrorInvalidConfiguration;
+    LOSSY_LAUNCH2(k_embed_grad_few, p.dy.bf16, p.grads.bf16, dim3((unsigned)blocks), dim3(kBlock),
+                  s, p, g);
+    return hipGetLastError();
+}
+
 hipError_t launch_embed_grad(const EmbedGradParams& p, void* ws, hipStream_t s) {
+    if (p.t <= kFewTokens) return launch_embed_grad_few(p, s);
     GradPlan g;
     grad_plan(p.n, p.t, p.h, p.tok.v, static_cast<uint8_t*>(ws), &g);
     const int u = p.dy.bf16 ? 8 : 4;
