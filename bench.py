@@ -16,7 +16,9 @@ and, for drift, stale replica packets read (lost gradient packets are never
 needed, so never counted).  Prints one JSON line on stdout.  Workloads
 smaller than 1 GiB get a 1 GiB scratch read between timed steps so that
 they are not served from the 256 MB memory-side cache; their throughput is
-then taken over the per-step events.
+then taken over the per-step events.  Where a workload's workers take their
+gradients on their own replicas (n8_layer16m_bf16_adam), these are taken before
+every step and timed apart (local_gradients_ms).
 """
 from __future__ import annotations
 
@@ -373,7 +375,9 @@ def main():
     # holding dirty lines that the timed step then has to write back.
     footprint = sum(t.numel() * t.element_size()
                     for t in (dev.grads, dev.replicas, dev.theta, dev.m, dev.v) if t is not None)
-    mall_flush = footprint < (1 << 30)
+    # A workload whose workers take their gradients on their replicas has them
+    # taken before every step, outside the step's events, and timed apart.
+    mall_flush = footprint < (1 << 30) and not w.layer
     scratch = torch.zeros(1 << 28, dtype=torch.float32, device="cuda") if mall_flush else None
     if mall_flush and args.mall_flush == "read":
         from paper_2507_07114_amd import probe
@@ -387,7 +391,14 @@ def main():
     ends = [torch.cuda.Event(enable_timing=True) for _ in range(args.steps)]
     torch.cuda.synchronize()
     wall0 = time.perf_counter()
+    local_ev = []
     for j in range(args.steps):
+        if w.layer:
+            inputs = wl.draw_layer_inputs(w, args.warmup + j, dev.theta.device)
+            local_ev.append([torch.cuda.Event(enable_timing=True) for _ in range(2)])
+            local_ev[-1][0].record(stream)
+            dev.local_gradients(args.warmup + j, inputs)
+            local_ev[-1][1].record(stream)
         if mall_flush:
             flush(j)
         starts[j].record(stream)
@@ -396,7 +407,7 @@ def main():
     torch.cuda.synchronize()
     wall = time.perf_counter() - wall0
     ms = [s.elapsed_time(e) for s, e in zip(starts, ends)]
-    if mall_flush:
+    if mall_flush or w.layer:
         wall = sum(ms) / 1e3
     drift = ll.read_drift(dev.drift)
 
@@ -471,6 +482,12 @@ def main():
         },
         "cpu_baseline": cpu,
     }
+    if w.layer:
+        local = sorted(a.elapsed_time(b) for a, b in local_ev)
+        result["config"]["layer"] = w.layer
+        result["local_gradients_ms"] = {"min": round(local[0], 4),
+                                        "median": round(float(np.median(local)), 4),
+                                        "max": round(local[-1], 4)}
     print(json.dumps(result), flush=True)
 
 

@@ -17,7 +17,9 @@ import pytest
 import torch
 
 import paper_2507_07114_amd as ll
+import workloads as wl
 from oracle import local as ol
+from workloads import device as wd
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -608,3 +610,38 @@ def test_captured_gradients_replay_like_eager():
         torch.cuda.synchronize()
         for x, y in ((a.x, b.x), (a.q, b.q), (a.s, b.s), (a.dx, b.dx), (a.grads, b.grads)):
             assert torch.equal(x, y), rep
+
+
+@pytest.mark.parametrize("gdtype", ["bf16", "f32"])
+def test_layer_workload_takes_its_gradients_on_its_replicas(gdtype):
+    w = wl.scaled(wl.WORKLOADS["n8_layer16m_bf16_adam"], n=3, d=(50 + 24) * 72, packet=128,
+                  gdtype=gdtype, loss=dict(kind=wl.BERNOULLI, p=0.3),
+                  layer=dict(vocab=50, h=72, o=24, t=90))
+    dev = wd.DeviceState(w)
+    for step in range(3):
+        dev.fused(step)  # replicas drift apart
+        reps = np64(dev.replicas)
+        tok, dy = wl.draw_layer_inputs(w, step + 1, DEV)
+        dev.local_gradients(step + 1)
+        torch.cuda.synchronize()
+        w0 = 50 * 72
+        for i in range(3):
+            x = ol.embed(tok[i].tolist(), reps[i, :w0].reshape(50, 72), 0, 1.0)
+            xq = ol.unpack(*ol.pack(x))
+            g = np64(dy[i])
+            want, size = ol.wgrad(g, xq, 1.0)
+            got = np64(dev.grads[i, w0:w.d]).reshape(24, 72)
+            terms = 3 if gdtype == "f32" else 1
+            u = half_step(wl.torch_dtype(gdtype))
+            assert (np.abs(got - want) <= 1.01 * ((2 * terms * 90 + 2) * U * size
+                                                  + u * np.abs(want))).all()
+            want, count, size = ol.embed_grad(tok[i].tolist(), np64(dev.dx[i]), 50, 0, 1.0)
+            got = np64(dev.grads[i, :w0]).reshape(50, 72)
+            assert (np.abs(got - want) <= 1.01 * ((count[:, None] + 2) * U * size
+                                                  + u * np.abs(want))).all()
+            ref, mag = g @ reps[i, w0:w.d].reshape(24, 72), np.abs(g) @ np.abs(
+                reps[i, w0:w.d].reshape(24, 72))
+            assert (np.abs(np64(dev.dx[i]) - ref) <= 1.01 * (2 * 24 * U * mag
+                                                             + u * np.abs(ref))).all()
+    assert not torch.equal(dev.replicas[0], dev.replicas[1])
+    assert ll.read_drift(dev.drift)["max_abs"] > 0

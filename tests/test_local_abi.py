@@ -171,3 +171,19 @@ def test_binding_refuses_tensors_that_do_not_fit():
         with pytest.raises(ValueError):
             f()
             print(f"call {k} was not refused")
+
+
+def test_layer_workload_inputs():
+    import workloads as wl
+    w = wl.WORKLOADS["n8_layer16m_bf16_adam"]
+    assert (w.layer["vocab"] + w.layer["o"]) * w.layer["h"] == w.d
+    w = wl.scaled(w, n=2, layer=dict(vocab=100, h=8, o=5, t=4000))
+    a, b = wl.draw_layer_inputs(w, 3), wl.draw_layer_inputs(w, 3)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert not torch.equal(a[0], wl.draw_layer_inputs(w, 4)[0])
+    assert a[0].dtype == torch.int32 and tuple(a[0].shape) == (2, 4000)
+    assert int(a[0].min()) >= 0 and int(a[0].max()) < 100
+    assert a[1].dtype == torch.bfloat16 and tuple(a[1].shape) == (2, 4000, 5)
+    p0 = (1 / 2.7) / sum(1 / (k + 2.7) for k in range(100))  # the commonest id
+    share = float((a[0] == 0).float().mean())
+    assert abs(share - p0) < 5 * (p0 * (1 - p0) / 8000) ** 0.5

@@ -36,7 +36,8 @@ class Workload:
     d       elements of the owned shard
     packet  elements per packet L; P = ceil(d / L), the last may be short
     gdtype  gradient row dtype; the replica dtype is the same
-    grad    gradient distribution: ("normal", std) or ("student_t", dof, scale)
+    grad    gradient distribution: ("normal", std) or ("student_t", dof, scale), or
+            ("layer", std): the gradients of `layer` for output gradients of that std
     loss    loss-process parameters (kind, p or Gilbert-Elliott rates)
     opt     optimizer kind and hyper-parameters
     steps   number of steps the configuration runs
@@ -53,6 +54,10 @@ class Workload:
     theta_std: float = 0.02
     drift_every_step: bool = False
     seed: int = 0
+    # What the shard holds, for workers that take their gradients on their own
+    # replicas (Section 3 step (1)): an embedding of vocab x h, then a linear layer
+    # of o x h on its output; t tokens a worker and step.
+    layer: Optional[dict] = None
 
     @property
     def num_packets(self) -> int:
@@ -106,6 +111,15 @@ WORKLOADS = {
         opt=dict(kind=SGD, lr=1e-3, momentum=0.0, beta1=0.0, beta2=0.0, eps=0.0),
         steps=200, drift_every_step=True),
 }
+
+# N=8 workers, an embedding and a linear layer in 16 Mi bf16 elements, each
+# worker's gradient taken on its own replica.
+WORKLOADS["n8_layer16m_bf16_adam"] = Workload(
+    name="n8_layer16m_bf16_adam", n=8, d=16_777_216, packet=2048, gdtype=BF16,
+    grad=("layer", 1e-3),
+    loss=dict(kind=BERNOULLI, p=0.01),
+    opt=dict(ADAM_DEFAULT), steps=10,
+    layer=dict(vocab=4096, h=2048, o=4096, t=2048))
 
 METRIC_WORKLOAD = "n64_llama7b_shard_bf16_adam"
 
@@ -180,6 +194,19 @@ def draw_grads(w: Workload, step: int, device="cpu", ld: Optional[int] = None,
     return out
 
 
+def draw_layer_inputs(w: Workload, step: int, device="cpu"):
+    """(tokens [N][t] int32, output gradients [N][t][o]) of step `step`: ids with
+    a language's frequencies, p(id) ~ 1 / (id + 2.7), and N(0, std^2)."""
+    l = w.layer
+    g = _gen(device, w.seed, 500_000 + step)
+    p = 1.0 / (torch.arange(l["vocab"], dtype=torch.float64) + 2.7)
+    cdf = (p / p.sum()).cumsum(0).to(device)
+    u = torch.rand(w.n * l["t"], generator=g, device=device, dtype=torch.float64)
+    tokens = torch.searchsorted(cdf, u).clamp_max(l["vocab"] - 1).to(torch.int32)
+    dy = torch.randn((w.n, l["t"], l["o"]), generator=g, device=device)
+    return tokens.view(w.n, l["t"]), (dy * float(w.grad[1])).to(torch_dtype(w.gdtype))
+
+
 def initial_replicas(theta0: torch.Tensor, w: Workload, ld: Optional[int] = None,
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Replica rows [N][ld]: every worker starts from the same copy of theta0
@@ -216,7 +243,7 @@ def describe(w: Workload) -> dict:
 
 __all__ = [
     "Workload", "WORKLOADS", "METRIC_WORKLOAD", "scaled", "draw_theta0",
-    "draw_grads", "initial_replicas", "packet_sample", "torch_dtype",
+    "draw_grads", "draw_layer_inputs", "initial_replicas", "packet_sample", "torch_dtype",
     "bf16_bits", "describe", "F32", "BF16", "SGD", "MOMENTUM", "ADAM",
     "BERNOULLI", "GILBERT_ELLIOTT",
 ]
