@@ -87,14 +87,23 @@ struct Sorted {
     }
 };
 
+// Table rows dealt out to workgroups: kRowUnits units, of a few whole rows or a
+// piece of a wide one.  Zeros alone, 8 workers' 25,695 rows of 4096 bf16 columns,
+// us: 512 units 274 (6.1 TB/s), 256 323, 1024 313.
+constexpr uint32_t kRowUnits = 512;
+
+struct RowBlocks {
+    int rows;               // table rows of a workgroup, at most 64
+    int64_t groups, spans;  // groups of rows of a worker, workgroups of a group
+    FlatRows units;         // units of a table row
+};
+
 struct GradPlan {
     Sorted s;
     float* part;    // [n][chunks][2][h] partial sums
     int chunk;      // sorted tokens of a wavefront
     int64_t chunks, strips, chunk_blocks;
-    int zero_rows;        // table rows of a workgroup that stores zeros, at most 64
-    int64_t zero_blocks;  // such workgroups of a worker
-    FlatRows units;       // 16-byte units of a table row
+    RowBlocks rows;
 };
 
 __global__ __launch_bounds__(kSortThreads) void k_token_sort(int64_t t, const int32_t* lengths,
@@ -218,14 +227,6 @@ __global__ __launch_bounds__(kSortThreads) void k_token_sort(int64_t t, const in
 // 261 / 299, one worker's 256 of 32000 x 4096 45 / 56, 200 of 1000 x 2048 9 / 16, 256
 // of 50 x 512 (4 workers) 13 / 16; 500 of 60000 x 128 (2 workers) 60 / 23.
 constexpr int kFewTokens = 256;
-constexpr uint32_t kFewUnits = 512;  // units of a workgroup
-
-struct FewPlan {
-    int rows;                // table rows of a workgroup, at most 64
-    int64_t groups, spans;   // such groups of a worker, workgroups of a group
-    FlatRows units;          // units of a table row
-};
-
 // One wavefront of step 2.  U columns a lane; rows and places of the chunk lie
 // one to a lane.
 template <class Y, class G>
@@ -293,26 +294,32 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradParams& p, const GradPl
     }
 }
 
-// A workgroup's rows that no token names: 8 KiB, or a row, 4 KiB at a time (8
-// workers' 25,695 rows of 4096 bf16 columns, no tokens: 300 us; 16 KiB 322, 64
-// KiB 345).  The counts come first, one to a lane, so that nothing stands between
-// the stores.
-template <class G>
+// Zeros for a workgroup's table rows that no token names.  Every lane has its
+// units' counts first, so that nothing stands between the stores.
+template <class Y, class G>
 __device__ __forceinline__ void zero_rows(const EmbedGradParams& p, const GradPlan& g, int64_t b) {
     typedef typename G::T GT;
-    constexpr int U = 16 / (int)sizeof(GT);
-    const int i = (int)(b / g.zero_blocks);
-    const int64_t r0 = (b - i * g.zero_blocks) * g.zero_rows;
-    const int rows = (int)(p.tok.v - r0 < g.zero_rows ? p.tok.v - r0 : g.zero_rows);
-    const int lane = threadIdx.x % kWave;
-    const uint64_t empty = __ballot(lane < rows && g.s.count[g.s.at(i, r0 + lane)] == 0);
+    constexpr int U = unit_of<Y, G>(), kTurns = kRowUnits / kBlock;
+    const int64_t span = b % g.rows.spans, group = b / g.rows.spans;
+    const int i = (int)(group / g.rows.groups);
+    const int64_t r0 = (group - i * g.rows.groups) * g.rows.rows;
+    const int rows = (int)(p.tok.v - r0 < g.rows.rows ? p.tok.v - r0 : g.rows.rows);
+    const uint32_t all = rows * g.rows.units.units;
+    const uint32_t u0 = (uint32_t)span * kRowUnits + threadIdx.x;
+    int count[kTurns];
+#pragma unroll
+    for (int a = 0; a < kTurns; ++a) {
+        const uint32_t u = u0 + a * kBlock;
+        count[a] = u < all ? g.s.count[g.s.at(i, r0 + flat_row(g.rows.units, u))] : 1;
+    }
     GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + r0 * p.h;
-    const uint32_t units = rows * g.units.units;
     const float zero[U] = {};
-    for (uint32_t u = threadIdx.x; u < units; u += kBlock) {
-        const uint32_t r = flat_row(g.units, u);
-        if (!(empty >> r & 1)) continue;
-        const int64_t c0 = (int64_t)(u - r * g.units.units) * U;
+#pragma unroll
+    for (int a = 0; a < kTurns; ++a) {
+        if (count[a]) continue;
+        const uint32_t u = u0 + a * kBlock;
+        const uint32_t r = flat_row(g.rows.units, u);
+        const int64_t c0 = (int64_t)(u - r * g.rows.units.units) * U;
         store_unit<GT, U, true>(grads + r * p.h + c0, p.h - c0, zero);
     }
 }
@@ -320,7 +327,7 @@ __device__ __forceinline__ void zero_rows(const EmbedGradParams& p, const GradPl
 template <class Y, class G>
 __global__ __launch_bounds__(kBlock, 8) void k_embed_grad(EmbedGradParams p, GradPlan g) {
     if (blockIdx.x >= g.chunk_blocks) {
-        zero_rows<G>(p, g, blockIdx.x - g.chunk_blocks);
+        zero_rows<Y, G>(p, g, blockIdx.x - g.chunk_blocks);
         return;
     }
     const int64_t w = (int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave;
@@ -387,7 +394,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, G
 // 8 KiB (or a piece of a wide row), looks all the worker's tokens through, keeps
 // those of its rows in order, and each lane adds up its unit's.
 template <class Y, class G>
-__global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, FewPlan g) {
+__global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, RowBlocks g) {
     typedef typename Y::T YT;
     typedef typename G::T GT;
     constexpr int U = unit_of<Y, G>();
@@ -443,8 +450,8 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Fe
     const YT* dy = static_cast<const YT*>(p.dy.p) + (int64_t)i * p.t * p.dy.ld;
     GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + r0 * p.h;
     const uint32_t all = rows * g.units.units;
-    const uint32_t u0 = (uint32_t)span * kFewUnits;
-    const uint32_t u1 = all - u0 < kFewUnits ? all : u0 + kFewUnits;
+    const uint32_t u0 = (uint32_t)span * kRowUnits;
+    const uint32_t u1 = all - u0 < kRowUnits ? all : u0 + kRowUnits;
     for (uint32_t u = u0 + threadIdx.x; u < u1; u += kBlock) {
         const int r = (int)flat_row(g.units, u);
         const int64_t c0 = (int64_t)(u - r * g.units.units) * U, have = p.h - c0;
@@ -536,20 +543,23 @@ size_t embed_grad_workspace(int64_t n, int64_t t, int64_t h, int64_t v) {
     return grad_plan(n, t, h, v, nullptr, &g);
 }
 
-static hipError_t launch_embed_grad_few(const EmbedGradParams& p, hipStream_t s) {
-    FewPlan g;
-    const int64_t units = (p.h + 7) / 8, wide = (p.h + 3) / 4;
-    const int64_t row = p.dy.bf16 || p.grads.bf16 ? units : wide;
-    const int64_t rows = kFewUnits / row;
-    // fewer where that leaves fewer workgroups than two to a compute unit
-    const int64_t few = p.n * p.tok.v / 512, most = rows < few ? rows : few;
-    g.rows = (int)(most < 1 ? 1 : (most > kWave ? kWave : most));
-    g.groups = (p.tok.v + g.rows - 1) / g.rows;
-    g.spans = (g.rows * row + kFewUnits - 1) / kFewUnits;
+// kRowUnits units to a workgroup, fewer rows where that leaves fewer workgroups
+// than two to a compute unit.
+static bool row_blocks(const EmbedGradParams& p, RowBlocks* g) {
+    const int64_t row = p.dy.bf16 || p.grads.bf16 ? (p.h + 7) / 8 : (p.h + 3) / 4;
+    const int64_t fit = kRowUnits / row, few = p.n * p.tok.v / 512, rows = fit < few ? fit : few;
+    g->rows = (int)(rows < 1 ? 1 : (rows > kWave ? kWave : rows));
+    g->groups = (p.tok.v + g->rows - 1) / g->rows;
+    g->spans = (g->rows * row + kRowUnits - 1) / kRowUnits;
     dim3 unused;
+    return flat_rows(g->rows, row, 1, &g->units, &unused);
+}
+
+static hipError_t launch_embed_grad_few(const EmbedGradParams& p, hipStream_t s) {
+    RowBlocks g;
+    if (!row_blocks(p, &g)) return hipErrorInvalidConfiguration;
     const int64_t blocks = p.n * g.groups * g.spans;
-    if (!flat_rows(g.rows, row, 1, &g.units, &unused) || blocks > 0xFFFFFFFFll / kBlock)
-        return hipErrorInvalidConfiguration;
+    if (blocks > 0xFFFFFFFFll / kBlock) return hipErrorInvalidConfiguration;
     LOSSY_LAUNCH2(k_embed_grad_few, p.dy.bf16, p.grads.bf16, dim3((unsigned)blocks), dim3(kBlock),
                   s, p, g);
     return hipGetLastError();
@@ -564,13 +574,8 @@ hipError_t launch_embed_grad(const EmbedGradParams& p, void* ws, hipStream_t s) 
     g.chunk_blocks = (p.n * g.chunks * g.strips + 3) / 4;
     int64_t blocks = g.chunk_blocks;
     if (!p.accumulate) {
-        const int64_t units = (p.h + (p.grads.bf16 ? 7 : 3)) / (p.grads.bf16 ? 8 : 4);
-        const int64_t rows = 512 / units;
-        g.zero_rows = (int)(rows < 1 ? 1 : (rows > kWave ? kWave : rows));
-        g.zero_blocks = (p.tok.v + g.zero_rows - 1) / g.zero_rows;
-        dim3 unused;
-        if (!flat_rows(g.zero_rows, units, 1, &g.units, &unused)) return hipErrorInvalidConfiguration;
-        blocks += p.n * g.zero_blocks;
+        if (!row_blocks(p, &g.rows)) return hipErrorInvalidConfiguration;
+        blocks += p.n * g.rows.groups * g.rows.spans;
     }
     const int64_t sorts = (int64_t)p.n << g.s.log_slices;
     const int64_t joins = (p.n * g.chunks * ((p.h + 255) / 256) + 3) / 4;
