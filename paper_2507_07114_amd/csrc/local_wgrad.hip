@@ -182,10 +182,17 @@ __device__ __forceinline__ void put_sums(const WgradParams& p, int i, int64_t o,
     store_unit<GT, U, true>(d, have, v);
 }
 
+// Bytes of LDS of a TO x TH tile.
+template <int TO, int TH>
+constexpr int lds_bytes() {
+    return kStages * kStepT * 2 * (TO + TH);
+}
+
 // A workgroup of WO x WH wavefronts owns a TO x TH tile of D over a run of
-// tokens.  TAILS: o or h is not a multiple of 8.
+// tokens.  TAILS: the tile's width or height is not a multiple of 8.
 template <class Y, class G, int TO, int TH, int WO, int WH, bool TAILS>
-__device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan& g) {
+__device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan& g, Tile tile,
+                                           int64_t ticket, int run, bool apart, uint8_t* lds) {
     typedef typename Y::T YT;
     constexpr int kThreads = WO * WH * kWave;
     constexpr int NI = TO / WO / 32, MI = TH / WH / 32;  // 32 x 32 products of a wavefront
@@ -194,13 +201,6 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     constexpr int kStageY = kStepT * kRowY, kStageX = kStepT * kRowX;
     constexpr int kStage = kStageY + kStageX, kPair = 2 * kStage;  // powers of two
     typedef Staged<Y, TO, TH, kThreads> Stage;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kStages * kStage];
-
-    const bool apart = g.runs > 1 && blockIdx.x >= g.whole;
-    const int64_t ticket = apart ? blockIdx.x - g.whole : blockIdx.x;
-    const int run = apart ? (int)(ticket % g.runs) : 0;
-    const Tile tile =
-        tile_at<TO, TH>(g, apart ? g.whole + ticket / g.runs : spread(ticket, g.whole));
     const int i = tile.i;
     const int64_t o0 = tile.o0, h0 = tile.h0;
     const int64_t m = batch_len(p.lengths, i, p.t);
@@ -450,14 +450,38 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     }
 }
 
+// The tile of a workgroup.  TAILS: o or h is not a multiple of 8; the tiles that
+// end there take a slower loop (4097 x 4099 x 4096 tokens: 158 us, 200 where all
+// tiles are 128 x 128; 4096 x 4096 with no such tile 116), which the others need not.
+template <class Y, class G, int EDGE, int WO, int WH, bool TAILS>
+__device__ __forceinline__ void wgrad_block(const WgradParams& p, const WgradPlan& g, uint8_t* lds) {
+    const bool apart = g.runs > 1 && blockIdx.x >= g.whole;
+    const int64_t ticket = apart ? blockIdx.x - g.whole : blockIdx.x;
+    const int run = apart ? (int)(ticket % g.runs) : 0;
+    const Tile tile =
+        tile_at<EDGE, EDGE>(g, apart ? g.whole + ticket / g.runs : spread(ticket, g.whole));
+    if (TAILS && ((p.o % 8 && p.o - tile.o0 < EDGE) || (p.h % 8 && p.h - tile.h0 < EDGE)))
+        wgrad_tile<Y, G, EDGE, EDGE, WO, WH, true>(p, g, tile, ticket, run, apart, lds);
+    else
+        wgrad_tile<Y, G, EDGE, EDGE, WO, WH, false>(p, g, tile, ticket, run, apart, lds);
+}
+
 template <class Y, class G>
 __global__ __launch_bounds__(512, 1) void k_act_wgrad_256(WgradParams p, WgradPlan g) {
-    wgrad_tile<Y, G, 256, 256, 2, 4, false>(p, g);
+    __shared__ __attribute__((aligned(16))) uint8_t lds[lds_bytes<256, 256>()];
+    wgrad_block<Y, G, 256, 2, 4, false>(p, g, lds);
+}
+
+template <class Y, class G>
+__global__ __launch_bounds__(512, 1) void k_act_wgrad_256_tails(WgradParams p, WgradPlan g) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[lds_bytes<256, 256>()];
+    wgrad_block<Y, G, 256, 2, 4, true>(p, g, lds);
 }
 
 template <class Y, class G>
 __global__ __launch_bounds__(256, 2) void k_act_wgrad_128(WgradParams p, WgradPlan g) {
-    wgrad_tile<Y, G, 128, 128, 2, 2, true>(p, g);
+    __shared__ __attribute__((aligned(16))) uint8_t lds[lds_bytes<128, 128>()];
+    wgrad_block<Y, G, 128, 2, 2, true>(p, g, lds);
 }
 
 // Sum of the runs of the tiles that were summed apart, in order.
@@ -519,7 +543,9 @@ void wgrad_plan(int64_t n, int64_t t, int64_t o, int64_t h, bool bf16, WgradPlan
     const double cost = bf16 ? 1.0 : 3.75;
     double best = 0.0;
     for (int edge = 256; edge >= 128; edge /= 2) {
-        if (edge == 256 && (o % 8 || h % 8)) continue;  // its kernel has no odd columns
+        // with tails the large tile of fp32 dy has too few registers (2 x 2000
+        // tokens of 3001 x 1777: 267 us, 218 by small tiles)
+        if (edge == 256 && !bf16 && (o % 8 || h % 8)) continue;
         const int64_t tiles_o = (o + edge - 1) / edge, tiles_h = (h + edge - 1) / edge;
         const int64_t tiles = n * tiles_o * tiles_h;
         const int64_t places = edge == 256 ? kCus : 2 * kCus;
@@ -567,10 +593,16 @@ hipError_t launch_act_wgrad(const WgradParams& p, void* ws, hipStream_t s) {
     const int64_t blocks = g.whole + g.rest * g.runs;
     if (blocks > 0xFFFFFFFFll / 512) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks);
-    if (g.edge == 256)
+    if (g.edge == 256 && (p.o % 8 || p.h % 8)) {  // bf16 dy
+        if (p.grads.bf16)
+            hipLaunchKernelGGL((k_act_wgrad_256_tails<El16, El16>), grid, dim3(512), 0, s, p, g);
+        else
+            hipLaunchKernelGGL((k_act_wgrad_256_tails<El16, El32>), grid, dim3(512), 0, s, p, g);
+    } else if (g.edge == 256) {
         LOSSY_LAUNCH2(k_act_wgrad_256, p.dy.bf16, p.grads.bf16, grid, dim3(512), s, p, g);
-    else
+    } else {
         LOSSY_LAUNCH2(k_act_wgrad_128, p.dy.bf16, p.grads.bf16, grid, dim3(256), s, p, g);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.runs == 1) return e;
     const dim3 join((unsigned)(g.rest * (g.edge * g.edge / 4 / kBlock)));
