@@ -23,7 +23,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) i16x4 LdsQuad;
 
 constexpr int kStepT = 32;    // tokens of a step
-constexpr int kStages = 4;    // steps whose tiles are in LDS, as two pairs
 
 // The tiles of all workers in order; the first `whole` are summed by a workgroup
 // each, the other `rest` by `runs` workgroups over run_t tokens each, whose
@@ -139,11 +138,6 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t step_rows(const uint8_t* p, in
 // 2^31 bytes (checked at the entry point).
 constexpr uint32_t kNowhere = 0x80000000u;
 
-template <int N>
-struct Part {
-    static constexpr int value = N;
-};
-
 struct Tile {
     int i;           // worker
     int64_t o0, h0;  // corner
@@ -182,10 +176,11 @@ __device__ __forceinline__ void put_sums(const WgradParams& p, int i, int64_t o,
     store_unit<GT, U, true>(d, have, v);
 }
 
-// Bytes of LDS of a TO x TH tile.
-template <int TO, int TH>
+// Bytes of LDS of an EDGE x EDGE tile: four steps of bf16 dy and codes, or two of
+// the three terms of fp32 dy and the codes.
+template <int EDGE>
 constexpr int lds_bytes() {
-    return kStages * kStepT * 2 * (TO + TH);
+    return 2 * 4 * kStepT * 2 * EDGE;
 }
 
 // A workgroup of WO x WH wavefronts owns a TO x TH tile of D over a run of
@@ -199,16 +194,17 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     constexpr int kTerms = sizeof(YT) == 4 ? 3 : 1;
     constexpr int kRowY = TO * 2, kRowX = TH * 2;  // bytes of a tile row
     constexpr int kStageY = kStepT * kRowY, kStageX = kStepT * kRowX;
-    constexpr int kStage = kStageY + kStageX, kPair = 2 * kStage;  // powers of two
+    constexpr int kAllY = kTerms * kStageY, kStage = kAllY + kStageX;
+    // half of the LDS, a power of two: two stages of bf16 dy, one of fp32 dy
+    constexpr int kFlip = kTerms == 1 ? 2 * kStage : kStage;
+    static_assert(TO == TH && 2 * kFlip == lds_bytes<TO>(), "LDS");
     typedef Staged<Y, TO, TH, kThreads> Stage;
     const int i = tile.i;
     const int64_t o0 = tile.o0, h0 = tile.h0;
     const int64_t m = batch_len(p.lengths, i, p.t);
     const int64_t t0 = run * g.run_t;
     const int64_t t1 = apart && t0 + g.run_t < m ? t0 + g.run_t : m;
-    // tokens in pairs of blocks; loads past the run's end give zeros
     const int left = t1 > t0 ? (int)(t1 - t0) : 0;
-    const int pairs = (left + 2 * kStepT - 1) / (2 * kStepT);
 
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     // staging: thread -> token row and 8 columns; the columns past the last
@@ -234,20 +230,18 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     const bool ywhole = !(ysplit && ycol == ywidth / 8 * 8);
     const bool xwhole = !(xsplit && xcol == xwidth / 8 * 8);
 
-    // Loads of the next step's tiles, one piece a call (y rows, then x rows);
-    // the step's tokens are done with `last`.
+    // Loads of the next step's tiles, one piece a call (y rows, then x rows); past
+    // the run's end they give zeros.
     __amdgpu_buffer_rsrc_t yr, xr, sr;
-    auto open_stage = [&](bool last) {
+    auto open_stage = [&] {
         const int rows = rows_left < kStepT ? rows_left : kStepT;
         yr = step_rows(ynext, rows, yld, ywidth * (int)sizeof(YT));
         xr = step_rows(xnext, rows, xld, xwidth);
         sr = step_rows(snext, rows, sld, (xwidth + kActGroup - 1) / kActGroup);
-        if (last) {
-            ynext += (int64_t)kStepT * yld;
-            xnext += (int64_t)kStepT * xld;
-            snext += (int64_t)kStepT * sld;
-            rows_left -= kStepT;
-        }
+        ynext += (int64_t)kStepT * yld;
+        xnext += (int64_t)kStepT * xld;
+        snext += (int64_t)kStepT * sld;
+        rows_left -= kStepT;
     };
     constexpr int kPieces = Stage::kPassY + Stage::kPassX;
     auto load_piece = [&](Stage& r, int piece) {
@@ -267,13 +261,13 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
             }
         }
     };
-    auto load_stage = [&](Stage& r, bool last) {
-        open_stage(last);
+    auto load_stage = [&](Stage& r) {
+        open_stage();
 #pragma unroll
         for (int a = 0; a < kPieces; ++a) load_piece(r, a);
     };
-    // LDS places of what a thread stages, in the current pair of stages; a
-    // change of pair flips one bit
+    // LDS places of what a thread stages, in one half of the LDS; the other's
+    // differ in one bit
     auto place = [](int k, int col, int row_bytes) {
         return k * row_bytes + unit_at(k, col / 16) * 32 + col % 16 * 2;
     };
@@ -283,33 +277,42 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
         yput[a] = place(yrow + a * (kStepT / Stage::kPassY), ycol, kRowY);
 #pragma unroll
     for (int a = 0; a < Stage::kPassX; ++a)
-        xput[a] = kStageY + place(xrow + a * (kStepT / Stage::kPassX), xcol, kRowX);
-    int ytput = place(trow, ytcol, kRowY), xtput = kStageY + place(trow, xtcol, kRowX);
-    // store a piece into the pair that `pair` says (0 or kPair), its stage `half`
-    auto store_piece = [&](const Stage& r, auto part, int pair, int half, int piece) {
-        constexpr int kPart = decltype(part)::value;
-        uint8_t* to = lds + half * kStage;
+        xput[a] = kAllY + place(xrow + a * (kStepT / Stage::kPassX), xcol, kRowX);
+    const int ytput = place(trow, ytcol, kRowY), xtput = kAllY + place(trow, xtcol, kRowX);
+    // store a piece into the half that `flip` says (0 or kFlip), stage `stage` of it
+    auto store_piece = [&](const Stage& r, int flip, int stage, int piece) {
+        uint8_t* to = lds + stage * kStage;
         if (piece < Stage::kPassY) {
-            if (!TAILS || ywhole)
-                *reinterpret_cast<u32x4*>(to + (yput[piece] ^ pair)) =
-                    r.y[piece].template terms<kPart>();
+            if (!TAILS || ywhole) {
+                u32x4* y = reinterpret_cast<u32x4*>(to + (yput[piece] ^ flip));
+                y[0] = r.y[piece].template terms<0>();
+                if (kTerms == 3) {
+                    y[kStageY / 16] = r.y[piece].template terms<1>();
+                    y[2 * kStageY / 16] = r.y[piece].template terms<2>();
+                }
+            }
         } else {
             const int a = piece - Stage::kPassY;
             if (!TAILS || xwhole)
-                *reinterpret_cast<u32x4*>(to + (xput[a] ^ pair)) = restore8(r.x[a], r.s[a]);
+                *reinterpret_cast<u32x4*>(to + (xput[a] ^ flip)) = restore8(r.x[a], r.s[a]);
         }
         if (piece == kPieces - 1) {
-            if (ysplit)
-                *reinterpret_cast<uint16_t*>(to + (ytput ^ pair)) =
-                    (uint16_t)Chunk8<Y>::template term1<kPart>(r.ytail);
+            if (ysplit) {
+                uint16_t* y = reinterpret_cast<uint16_t*>(to + (ytput ^ flip));
+                y[0] = (uint16_t)Chunk8<Y>::template term1<0>(r.ytail);
+                if (kTerms == 3) {
+                    y[kStageY / 2] = (uint16_t)Chunk8<Y>::template term1<1>(r.ytail);
+                    y[2 * kStageY / 2] = (uint16_t)Chunk8<Y>::template term1<2>(r.ytail);
+                }
+            }
             if (xsplit)
-                *reinterpret_cast<uint16_t*>(to + (xtput ^ pair)) =
+                *reinterpret_cast<uint16_t*>(to + (xtput ^ flip)) =
                     (uint16_t)restore8(u32x2{r.xtail, 0}, r.stail).x;
         }
     };
-    auto store_stage = [&](const Stage& r, auto part, int pair, int half) {
+    auto store_stage = [&](const Stage& r, int flip, int stage) {
 #pragma unroll
-        for (int a = 0; a < kPieces; ++a) store_piece(r, part, pair, half, a);
+        for (int a = 0; a < kPieces; ++a) store_piece(r, flip, stage, a);
     };
     auto barrier = [] {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -328,7 +331,7 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
                    lane % 4 * 8;
 #pragma unroll
     for (int a = 0; a < MI; ++a)
-        xaddr[a] = kStageY + frow * kRowX +
+        xaddr[a] = kAllY + frow * kRowX +
                    unit_at(frow, (wh + a * 32) / 16 + lane / 16 % 2) * 32 + lane % 4 * 8;
     auto fragment = [&](int at, int row_bytes) {
         uint8_t* q = lds + at;
@@ -339,70 +342,116 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
         __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
         return f;
     };
-    struct Frags {
-        bf16x8 y[NI], x[MI];
+    auto read_y = [&](int flip, int stage, int half, int term, int b) {
+        return fragment((yaddr[b] ^ flip) + stage * kStage + term * kStageY + half * 16 * kRowY,
+                        kRowY);
     };
-    // fragment b in the order of their use: x 0, all y, the other x
-    constexpr int kFrags = MI + NI;
-    auto read_frag = [&](Frags& f, int pair, int stage, int half, int b) {
-        if (b >= 1 && b <= NI)
-            f.y[b - 1] = fragment((yaddr[b - 1] ^ pair) + stage * kStage + half * 16 * kRowY, kRowY);
-        else
-            f.x[b ? b - NI : 0] = fragment((xaddr[b ? b - NI : 0] ^ pair) + stage * kStage +
-                                               half * 16 * kRowX, kRowX);
+    auto read_x = [&](int flip, int stage, int half, int b) {
+        return fragment((xaddr[b] ^ flip) + stage * kStage + half * 16 * kRowX, kRowX);
     };
     f32x16 acc[MI][NI] = {};
-    // Two steps s, s + 1 multiply one pair of stages, store tiles s + 2, s + 3 into
-    // the other and load tiles s + 4, s + 5 into the registers this frees.  The
-    // workgroup meets once, before the last quarter, whose fragments are then
-    // read: behind it the stored pair may be read and this one stored.  A
-    // wavefront issues an instruction every 4 cycles and a product takes 32, so
-    // reads, stores and loads are dealt out between the products.
-    Stage r[2];
-    Frags f0, f1;
-    load_stage(r[0], kTerms == 1);
-    load_stage(r[1], kTerms == 1);
-    store_stage(r[0], Part<0>(), 0, 0);
-    load_stage(r[0], true);
-    store_stage(r[1], Part<1 % kTerms>(), 0, 1);
-    load_stage(r[1], kTerms == 1);
-    barrier();
-#pragma unroll
-    for (int b = 0; b < kFrags; ++b) read_frag(f0, 0, 0, 0, b);
-    int pair = 0;
     constexpr int kProducts = MI * NI;
-    // half a step: its products, and after each its share of the next half's
-    // fragments and of the pieces to be stored or loaded
-    auto half = [&](const Frags& now, auto read, auto move) {
+    // The products of half a step's tokens (of one term).  A wavefront issues an
+    // instruction every 4 cycles and a product takes 32, so after each product
+    // comes a share of the `reads` next fragments and the `moves` pieces to be
+    // stored or loaded.
+    auto half = [&](const bf16x8 (&x)[MI], const bf16x8 (&y)[NI], int reads, auto read, int moves,
+                    auto move) {
 #pragma unroll
         for (int k = 0; k < kProducts; ++k) {
             acc[k / NI][k % NI] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                now.x[k / NI], now.y[k % NI], acc[k / NI][k % NI], 0, 0, 0);
+                x[k / NI], y[k % NI], acc[k / NI][k % NI], 0, 0, 0);
 #pragma unroll
-            for (int b = k * kFrags / kProducts; b < (k + 1) * kFrags / kProducts; ++b) read(b);
+            for (int b = k * reads / kProducts; b < (k + 1) * reads / kProducts; ++b) read(b);
 #pragma unroll
-            for (int a = k * kPieces / kProducts; a < (k + 1) * kPieces / kProducts; ++a) move(a);
+            for (int a = k * moves / kProducts; a < (k + 1) * moves / kProducts; ++a) move(a);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto two_steps = [&](auto part) {
-        constexpr int s = decltype(part)::value;
-        half(f0, [&](int b) { read_frag(f1, pair, 0, 1, b); },
-             [&](int a) { store_piece(r[0], Part<(s + 2) % kTerms>(), pair ^ kPair, 0, a); });
-        open_stage((s + 4) % kTerms == kTerms - 1);
-        half(f1, [&](int b) { read_frag(f0, pair, 1, 0, b); }, [&](int a) { load_piece(r[0], a); });
-        half(f0, [&](int b) { read_frag(f1, pair, 1, 1, b); },
-             [&](int a) { store_piece(r[1], Part<(s + 3) % kTerms>(), pair ^ kPair, 1, a); });
-        open_stage((s + 5) % kTerms == kTerms - 1);
+    if constexpr (kTerms == 1) {
+        // Two steps s, s + 1 multiply the stages of one half of the LDS, store
+        // tiles s + 2, s + 3 into the other and load tiles s + 4, s + 5 into the
+        // registers this frees.  The workgroup meets once, before the last
+        // quarter, whose fragments are then read: behind it the stored half may
+        // be read and this one stored.
+        constexpr int kFrags = MI + NI;
+        struct Frags {
+            bf16x8 x[MI], y[NI];
+        };
+        // fragment b in the order of their use: x 0, all y, the other x
+        auto read = [&](Frags& f, int flip, int stage, int part, int b) {
+            if (b >= 1 && b <= NI) f.y[b - 1] = read_y(flip, stage, part, 0, b - 1);
+            else f.x[b ? b - NI : 0] = read_x(flip, stage, part, b ? b - NI : 0);
+        };
+        Stage r[2];
+        Frags f0, f1;
+        load_stage(r[0]);
+        load_stage(r[1]);
+        store_stage(r[0], 0, 0);
+        load_stage(r[0]);
+        store_stage(r[1], 0, 1);
+        load_stage(r[1]);
         barrier();
-        pair ^= kPair;
-        half(f1, [&](int b) { read_frag(f0, pair, 0, 0, b); }, [&](int a) { load_piece(r[1], a); });
-    };
-    for (int k = 0; k < pairs; ++k) {
-        two_steps(Part<0>());
-        if (kTerms == 3) {
-            two_steps(Part<2>());
-            two_steps(Part<4>());
+#pragma unroll
+        for (int b = 0; b < kFrags; ++b) read(f0, 0, 0, 0, b);
+        int flip = 0;
+        for (int k = 0; k < left; k += 2 * kStepT) {
+            half(f0.x, f0.y, kFrags, [&](int b) { read(f1, flip, 0, 1, b); }, kPieces,
+                 [&](int a) { store_piece(r[0], flip ^ kFlip, 0, a); });
+            open_stage();
+            half(f1.x, f1.y, kFrags, [&](int b) { read(f0, flip, 1, 0, b); }, kPieces,
+                 [&](int a) { load_piece(r[0], a); });
+            half(f0.x, f0.y, kFrags, [&](int b) { read(f1, flip, 1, 1, b); }, kPieces,
+                 [&](int a) { store_piece(r[1], flip ^ kFlip, 1, a); });
+            open_stage();
+            barrier();
+            flip ^= kFlip;
+            half(f1.x, f1.y, kFrags, [&](int b) { read(f0, flip, 0, 0, b); }, kPieces,
+                 [&](int a) { load_piece(r[1], a); });
+        }
+    } else {
+        // A step multiplies the codes' fragments by the three terms' in turn,
+        // stores the next tile into the other half and loads the one after into
+        // the registers this frees; the workgroup meets before the last sixth.
+        Stage r;
+        bf16x8 x0[MI], x1[MI], y0[NI], y1[NI];
+        load_stage(r);
+        store_stage(r, 0, 0);
+        load_stage(r);
+        barrier();
+#pragma unroll
+        for (int b = 0; b < MI; ++b) x0[b] = read_x(0, 0, 0, b);
+#pragma unroll
+        for (int b = 0; b < NI; ++b) y0[b] = read_y(0, 0, 0, 0, b);
+        int flip = 0;
+        constexpr int kFirst = (kPieces + 2) / 3, kThen = 2 * kFirst < kPieces ? kFirst : kPieces - kFirst;
+        constexpr int kLast = kPieces - kFirst - kThen;  // pieces of three sixths
+        auto nothing = [](int) {};
+        for (int k = 0; k < left; k += kStepT) {
+            const int other = flip ^ kFlip;
+            half(x0, y0, NI, [&](int b) { y1[b] = read_y(flip, 0, 0, 1, b); }, kFirst,
+                 [&](int a) { store_piece(r, other, 0, a); });
+            half(x0, y1, NI, [&](int b) { y0[b] = read_y(flip, 0, 0, 2, b); }, kThen,
+                 [&](int a) { store_piece(r, other, 0, kFirst + a); });
+            half(x0, y0, NI + MI,
+                 [&](int b) {
+                     if (b < NI) y1[b] = read_y(flip, 0, 1, 0, b);
+                     else x1[b - NI] = read_x(flip, 0, 1, b - NI);
+                 },
+                 kLast, [&](int a) { store_piece(r, other, 0, kFirst + kThen + a); });
+            open_stage();
+            half(x1, y1, NI, [&](int b) { y0[b] = read_y(flip, 0, 1, 1, b); }, kFirst,
+                 [&](int a) { load_piece(r, a); });
+            half(x1, y0, NI, [&](int b) { y1[b] = read_y(flip, 0, 1, 2, b); }, kPieces - kFirst,
+                 [&](int a) { load_piece(r, kFirst + a); });
+            barrier();
+            flip = other;
+            half(x1, y1, NI + MI,
+                 [&](int b) {
+                     if (b < NI) y0[b] = read_y(flip, 0, 0, 0, b);
+                     else x0[b - NI] = read_x(flip, 0, 0, b - NI);
+                 },
+                 0, nothing);
         }
     }
 
@@ -410,7 +459,7 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     // Through LDS, a wavefront's own part of it, they become whole row pieces:
     // 32 rows at a time, padded by 16 bytes against bank conflicts.
     constexpr int kWide = MI * 32, kPadded = kWide + 4;
-    static_assert(kWide == 64 && WO * WH * 32 * kPadded * 4 <= kStages * kStage, "LDS of the end");
+    static_assert(kWide == 64 && WO * WH * 32 * kPadded * 4 <= 2 * kFlip, "LDS of the end");
     barrier();
     float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kPadded;
 #pragma unroll
@@ -468,19 +517,19 @@ __device__ __forceinline__ void wgrad_block(const WgradParams& p, const WgradPla
 
 template <class Y, class G>
 __global__ __launch_bounds__(512, 1) void k_act_wgrad_256(WgradParams p, WgradPlan g) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[lds_bytes<256, 256>()];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[lds_bytes<256>()];
     wgrad_block<Y, G, 256, 2, 4, false>(p, g, lds);
 }
 
 template <class Y, class G>
 __global__ __launch_bounds__(512, 1) void k_act_wgrad_256_tails(WgradParams p, WgradPlan g) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[lds_bytes<256, 256>()];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[lds_bytes<256>()];
     wgrad_block<Y, G, 256, 2, 4, true>(p, g, lds);
 }
 
 template <class Y, class G>
 __global__ __launch_bounds__(256, 2) void k_act_wgrad_128(WgradParams p, WgradPlan g) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[lds_bytes<128, 128>()];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[lds_bytes<128>()];
     wgrad_block<Y, G, 128, 2, 2, true>(p, g, lds);
 }
 
@@ -516,36 +565,37 @@ __global__ __launch_bounds__(kBlock) void k_act_wgrad_join(WgradParams p, WgradP
     else join_tile<G, 128>(p, g);
 }
 
-// Microseconds of a plan, from measurements on square layers of 256 to 4096 and
-// 64 to 8192 tokens.  A launch with its first loads and last stores takes 9
-// (256 x 256 tiles) or 6.7 (128 x 128); a step of 32 tokens 0.57 where few
-// compute units work and 0.80 where all do, or 0.35, 0.40 and, with two tiles
-// on a compute unit, 0.55; fp32 dy takes three steps of 1.25 times that.
-// Sums kept apart cost 3 and 0.27 a megabyte.  For 2048 x 2048 and 512 tokens
-// that gives 128 x 128 tiles in one run (12.1; two runs 33.5, 256 x 256 18.8),
-// for 8192 tokens 256 x 256 in four (77.4; one run 156.4, 128 x 128 89.8).
+// Microseconds of a plan, from measurements on square layers of 256 to 4096 and 64
+// to 8192 tokens: a launch with its first loads and last stores, and a step of 32
+// tokens where few compute units work, where each has a tile and, of 128 x 128
+// tiles, where each has two.  Sums kept apart cost 3 and 0.27 a megabyte.  bf16,
+// 2048 x 2048 and 512 tokens: 128 x 128 tiles in one run (12.1; two runs 33.5, 256 x
+// 256 18.8); 8192 tokens: 256 x 256 in four (77.4; one run 156.4, 128 x 128 89.8).
+// fp32, 2048 tokens: 128 x 128 in two (62.3; one 63.4, 256 x 256 in four 63.4).
 constexpr int64_t kCus = 256;
 
-double tiles_us(int edge, int64_t blocks, double steps) {
-    const int64_t places = edge == 256 ? kCus : 2 * kCus;
+struct TileCost {
+    double launch, few, one, two;
+};
+constexpr TileCost kCost[2][2] = {  // [bf16][256 x 256]
+    {{7.0, 0.83, 0.83, 1.40}, {11.0, 1.69, 2.30, 0.0}},
+    {{6.7, 0.35, 0.40, 0.55}, {9.0, 0.57, 0.80, 0.0}},
+};
+
+double tiles_us(const TileCost& c, int64_t places, int64_t blocks, int64_t steps) {
     const int64_t full = blocks / places, rest = blocks - full * places;
-    const double most = edge == 256 ? 0.80 : 0.55;
-    double last = 0.0;
-    if (rest > 0) {
-        if (edge == 256) last = 0.57 + 0.23 * rest / kCus;
-        else last = rest <= kCus ? 0.35 + 0.05 * rest / kCus : 0.55;
-    }
-    return steps * (full * most + last);
+    const double round = places > kCus ? c.two : c.one;
+    const double last = rest == 0      ? 0.0
+                        : rest <= kCus ? c.few + (c.one - c.few) * rest / kCus
+                                       : c.two;
+    return steps * (full * round + last);
 }
 
 void wgrad_plan(int64_t n, int64_t t, int64_t o, int64_t h, bool bf16, WgradPlan* g) {
     const int64_t steps = (t + kStepT - 1) / kStepT;
-    const double cost = bf16 ? 1.0 : 3.75;
     double best = 0.0;
     for (int edge = 256; edge >= 128; edge /= 2) {
-        // with tails the large tile of fp32 dy has too few registers (2 x 2000
-        // tokens of 3001 x 1777: 267 us, 218 by small tiles)
-        if (edge == 256 && !bf16 && (o % 8 || h % 8)) continue;
+        const TileCost& cost = kCost[bf16][edge == 256];
         const int64_t tiles_o = (o + edge - 1) / edge, tiles_h = (h + edge - 1) / edge;
         const int64_t tiles = n * tiles_o * tiles_h;
         const int64_t places = edge == 256 ? kCus : 2 * kCus;
@@ -555,9 +605,9 @@ void wgrad_plan(int64_t n, int64_t t, int64_t o, int64_t h, bool bf16, WgradPlan
             if (runs > 1 && (rest == 0 || rest * runs > 4 * kCus)) break;
             int64_t each = (steps + runs - 1) / runs;
             if (each < 1) each = 1;
-            double us = (edge == 256 ? 9.0 : 6.7) + tiles_us(edge, whole, cost * steps);
+            double us = cost.launch + tiles_us(cost, places, whole, steps);
             if (runs > 1)
-                us += tiles_us(edge, rest * runs, cost * each) + 3.0 +
+                us += tiles_us(cost, places, rest * runs, each) + 3.0 +
                       0.27e-6 * rest * runs * edge * edge * 4;
             if (g->edge && us >= best) continue;
             best = us;
@@ -593,11 +643,8 @@ hipError_t launch_act_wgrad(const WgradParams& p, void* ws, hipStream_t s) {
     const int64_t blocks = g.whole + g.rest * g.runs;
     if (blocks > 0xFFFFFFFFll / 512) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks);
-    if (g.edge == 256 && (p.o % 8 || p.h % 8)) {  // bf16 dy
-        if (p.grads.bf16)
-            hipLaunchKernelGGL((k_act_wgrad_256_tails<El16, El16>), grid, dim3(512), 0, s, p, g);
-        else
-            hipLaunchKernelGGL((k_act_wgrad_256_tails<El16, El32>), grid, dim3(512), 0, s, p, g);
+    if (g.edge == 256 && (p.o % 8 || p.h % 8)) {
+        LOSSY_LAUNCH2(k_act_wgrad_256_tails, p.dy.bf16, p.grads.bf16, grid, dim3(512), s, p, g);
     } else if (g.edge == 256) {
         LOSSY_LAUNCH2(k_act_wgrad_256, p.dy.bf16, p.grads.bf16, grid, dim3(512), s, p, g);
     } else {
