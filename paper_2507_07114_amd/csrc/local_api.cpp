@@ -96,6 +96,13 @@ PackView pack_view(const uint8_t* q, int64_t ld_q, const uint8_t* s, int64_t ld_
     return PackView{const_cast<uint8_t*>(q), ld_q, const_cast<uint8_t*>(s), ld_s};
 }
 
+// The launchers refuse a grid that does not fit as hipErrorInvalidConfiguration,
+// before any launch.
+int launched(hipError_t e, const char* fn) {
+    if (e == hipErrorInvalidConfiguration) return fail(LL_EINVAL, "%s: too many workgroups", fn);
+    return hip_check(e, fn);
+}
+
 hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 
 }  // namespace
@@ -125,7 +132,7 @@ int ll_embed(int32_t n, int64_t t, int64_t h, int64_t v, int64_t first, int32_t 
     p.table = row_view(rdtype, replicas, ld_r, offset);
     p.scale = scale;
     p.out = act_view(odtype, out, ld_o);
-    return hip_check(launch_embed(p, as_stream(stream)), "ll_embed");
+    return launched(launch_embed(p, as_stream(stream)), "ll_embed");
 }
 
 size_t ll_embed_grad_workspace_bytes(int32_t n, int64_t t, int64_t h, int64_t v) {
@@ -158,7 +165,7 @@ int ll_embed_grad(int32_t n, int64_t t, int64_t h, int64_t v, int64_t first, int
     p.scale = scale;
     p.grads = row_view(gdtype, grads, ld_g, offset);
     p.accumulate = accumulate != 0;
-    return hip_check(launch_embed_grad(p, workspace, as_stream(stream)), "ll_embed_grad");
+    return launched(launch_embed_grad(p, workspace, as_stream(stream)), "ll_embed_grad");
 }
 
 int ll_act_pack(int32_t n, int64_t t, int64_t h, const int32_t* lengths, int32_t xdtype,
@@ -173,7 +180,7 @@ int ll_act_pack(int32_t n, int64_t t, int64_t h, const int32_t* lengths, int32_t
     if ((r = check_act("x", x, ld_x, h, elem_bytes(xdtype)))) return r;
     if ((r = check_pack(q, ld_q, s, ld_s, h))) return r;
     PackParams p{n, t, h, lengths, act_view(xdtype, x, ld_x), pack_view(q, ld_q, s, ld_s)};
-    return hip_check(launch_act_pack(p, as_stream(stream)), "ll_act_pack");
+    return launched(launch_act_pack(p, as_stream(stream)), "ll_act_pack");
 }
 
 int ll_act_unpack(int32_t n, int64_t t, int64_t h, const int32_t* lengths, const uint8_t* q,
@@ -188,7 +195,7 @@ int ll_act_unpack(int32_t n, int64_t t, int64_t h, const int32_t* lengths, const
     if ((r = check_pack(q, ld_q, s, ld_s, h))) return r;
     if ((r = check_act("out", out, ld_o, h, elem_bytes(odtype)))) return r;
     PackParams p{n, t, h, lengths, act_view(odtype, out, ld_o), pack_view(q, ld_q, s, ld_s)};
-    return hip_check(launch_act_unpack(p, as_stream(stream)), "ll_act_unpack");
+    return launched(launch_act_unpack(p, as_stream(stream)), "ll_act_unpack");
 }
 
 size_t ll_act_wgrad_workspace_bytes(int32_t n, int64_t t, int64_t o, int64_t h) {
@@ -229,7 +236,7 @@ int ll_act_wgrad(int32_t n, int64_t t, int64_t o, int64_t h, const int32_t* leng
     p.scale = scale;
     p.grads = row_view(gdtype, grads, ld_g, offset);
     p.accumulate = accumulate != 0;
-    return hip_check(launch_act_wgrad(p, workspace, as_stream(stream)), "ll_act_wgrad");
+    return launched(launch_act_wgrad(p, workspace, as_stream(stream)), "ll_act_wgrad");
 }
 
 }  // extern "C"

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedParams p, int lanes) {
 //    strip of columns, whatever rows they belong to, so a row that takes half
 //    of all tokens is summed by many wavefronts.  A row whose tokens lie in
 //    one chunk is stored; the others leave fp32 partial sums.  More
-//    wavefronts of the launch store zeros in the rows that have no token.
+//    workgroups of the launch store zeros in the rows that have no token.
 // 3. k_embed_grad_join adds the partial sums of rows that cross chunks, in
 //    order.
 
@@ -226,7 +226,8 @@ __global__ __launch_bounds__(kSortThreads) void k_token_sort(int64_t t, const in
 // us against the three launches: 8 workers' 256 tokens of 25,695 x 4096 bf16
 // 261 / 299, one worker's 256 of 32000 x 4096 45 / 56, 200 of 1000 x 2048 9 / 16, 256
 // of 50 x 512 (4 workers) 13 / 16; 500 of 60000 x 128 (2 workers) 60 / 23.
-constexpr int kFewTokens = 256;
+constexpr int kFewTokens = kBlock;  // one to a thread
+
 // One wavefront of step 2.  U columns a lane; rows and places of the chunk lie
 // one to a lane.
 template <class Y, class G>
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
     typedef typename Y::T YT;
     typedef typename G::T GT;
     constexpr int U = unit_of<Y, G>();
-    constexpr int kWaves = kBlock / kWave, kEach = kFewTokens / kBlock;
+    constexpr int kWaves = kBlock / kWave;
     constexpr int kAhead = 4;  // tokens whose loads are in flight
     __shared__ uint16_t place[kFewTokens];
     __shared__ uint8_t owner[kFewTokens];
@@ -407,42 +408,24 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
     const int i = (int)(group / g.groups);
     const int64_t r0 = (group - i * g.groups) * g.rows;
     const int rows = (int)(p.tok.v - r0 < g.rows ? p.tok.v - r0 : g.rows);
-    const int m = (int)batch_len(p.lengths, i, p.t);
+    const int m = (int)batch_len(p.lengths, i, p.t), j = threadIdx.x;
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
 
-    // a wavefront looks kEach * 64 consecutive tokens through
-    const int j0 = w * kEach * kWave + lane;
-    int row[kEach], mine = 0;
-    uint64_t hits[kEach];
-    int64_t id[kEach];
-#pragma unroll
-    for (int a = 0; a < kEach; ++a) {
-        const int j = j0 + a * kWave;
-        id[a] = m > 0 ? token_id(p.tok, i, j < m ? j : m - 1) : 0;
-    }
-#pragma unroll
-    for (int a = 0; a < kEach; ++a) {
-        const int64_t at = j0 + a * kWave < m ? table_row(p.tok, id[a]) - r0 : -1;
-        row[a] = at >= 0 && at < rows ? (int)at : -1;
-        hits[a] = __ballot(row[a] >= 0);
-        mine += __popcll(hits[a]);
-    }
-    if (lane == 0) found[w] = mine;
+    // the tokens of these rows, in order of their places
+    const int64_t row = j < m ? table_row(p.tok, i, j) - r0 : -1;
+    const bool mine = row >= 0 && row < rows;
+    const uint64_t hits = __ballot(mine);
+    if (lane == 0) found[w] = __popcll(hits);
     __syncthreads();
-    int at = 0, total = 0;
+    int at = __popcll(hits & ((1ull << lane) - 1)), total = 0;
 #pragma unroll
     for (int a = 0; a < kWaves; ++a) {
         at += a < w ? found[a] : 0;
         total += found[a];
     }
-#pragma unroll
-    for (int a = 0; a < kEach; ++a) {
-        if (row[a] >= 0) {
-            const int k = at + __popcll(hits[a] & ((1ull << lane) - 1));
-            place[k] = (uint16_t)(j0 + a * kWave);
-            owner[k] = (uint8_t)row[a];
-        }
-        at += __popcll(hits[a]);
+    if (mine) {
+        place[at] = (uint16_t)j;
+        owner[at] = (uint8_t)row;
     }
     __syncthreads();
     if (total == 0 && p.accumulate) return;
@@ -451,7 +434,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
     GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + r0 * p.h;
     const uint32_t all = rows * g.units.units;
     const uint32_t u0 = (uint32_t)span * kRowUnits;
-    const uint32_t u1 = all - u0 < kRowUnits ? all : u0 + kRowUnits;
+    const uint32_t u1 = u0 + kRowUnits < all ? u0 + kRowUnits : all;
     for (uint32_t u = u0 + threadIdx.x; u < u1; u += kBlock) {
         const int r = (int)flat_row(g.units, u);
         const int64_t c0 = (int64_t)(u - r * g.units.units) * U, have = p.h - c0;
@@ -526,6 +509,28 @@ size_t grad_plan(int64_t n, int64_t t, int64_t h, int64_t v, uint8_t* ws, GradPl
     return at;
 }
 
+// kRowUnits units to a workgroup, fewer rows where that leaves fewer workgroups
+// than two to a compute unit.
+bool row_blocks(const EmbedGradParams& p, RowBlocks* g) {
+    const int64_t row = p.dy.bf16 || p.grads.bf16 ? (p.h + 7) / 8 : (p.h + 3) / 4;
+    const int64_t fit = kRowUnits / row, few = p.n * p.tok.v / 512, rows = fit < few ? fit : few;
+    g->rows = (int)(rows < 1 ? 1 : (rows > kWave ? kWave : rows));
+    g->groups = (p.tok.v + g->rows - 1) / g->rows;
+    g->spans = (g->rows * row + kRowUnits - 1) / kRowUnits;
+    dim3 unused;
+    return flat_rows(g->rows, row, 1, &g->units, &unused);
+}
+
+hipError_t launch_embed_grad_few(const EmbedGradParams& p, hipStream_t s) {
+    RowBlocks g;
+    if (!row_blocks(p, &g)) return hipErrorInvalidConfiguration;
+    const int64_t blocks = p.n * g.groups * g.spans;
+    if (blocks > 0xFFFFFFFFll / kBlock) return hipErrorInvalidConfiguration;
+    LOSSY_LAUNCH2(k_embed_grad_few, p.dy.bf16, p.grads.bf16, dim3((unsigned)blocks), dim3(kBlock),
+                  s, p, g);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_embed(const EmbedParams& p, hipStream_t s) {
@@ -541,28 +546,6 @@ size_t embed_grad_workspace(int64_t n, int64_t t, int64_t h, int64_t v) {
     if (t <= kFewTokens) return 0;
     GradPlan g;
     return grad_plan(n, t, h, v, nullptr, &g);
-}
-
-// kRowUnits units to a workgroup, fewer rows where that leaves fewer workgroups
-// than two to a compute unit.
-static bool row_blocks(const EmbedGradParams& p, RowBlocks* g) {
-    const int64_t row = p.dy.bf16 || p.grads.bf16 ? (p.h + 7) / 8 : (p.h + 3) / 4;
-    const int64_t fit = kRowUnits / row, few = p.n * p.tok.v / 512, rows = fit < few ? fit : few;
-    g->rows = (int)(rows < 1 ? 1 : (rows > kWave ? kWave : rows));
-    g->groups = (p.tok.v + g->rows - 1) / g->rows;
-    g->spans = (g->rows * row + kRowUnits - 1) / kRowUnits;
-    dim3 unused;
-    return flat_rows(g->rows, row, 1, &g->units, &unused);
-}
-
-static hipError_t launch_embed_grad_few(const EmbedGradParams& p, hipStream_t s) {
-    RowBlocks g;
-    if (!row_blocks(p, &g)) return hipErrorInvalidConfiguration;
-    const int64_t blocks = p.n * g.groups * g.spans;
-    if (blocks > 0xFFFFFFFFll / kBlock) return hipErrorInvalidConfiguration;
-    LOSSY_LAUNCH2(k_embed_grad_few, p.dy.bf16, p.grads.bf16, dim3((unsigned)blocks), dim3(kBlock),
-                  s, p, g);
-    return hipGetLastError();
 }
 
 hipError_t launch_embed_grad(const EmbedGradParams& p, void* ws, hipStream_t s) {

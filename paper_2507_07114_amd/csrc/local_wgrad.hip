@@ -204,7 +204,7 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     const int64_t m = batch_len(p.lengths, i, p.t);
     const int64_t t0 = run * g.run_t;
     const int64_t t1 = apart && t0 + g.run_t < m ? t0 + g.run_t : m;
-    const int left = t1 > t0 ? (int)(t1 - t0) : 0;
+    const uint32_t left = t1 > t0 ? (uint32_t)(t1 - t0) : 0;  // tokens, below 2^31
 
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     // staging: thread -> token row and 8 columns; the columns past the last
@@ -216,7 +216,7 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
         static_cast<const YT*>(p.dy.p) + (i * p.t + t0) * p.dy.ld + o0);
     const uint8_t* xnext = p.x.q + (i * p.t + t0) * p.x.ld_q + h0;
     const uint8_t* snext = p.x.s + (i * p.t + t0) * p.x.ld_s + h0 / kActGroup;
-    int rows_left = left;  // from the next step's first token on
+    int rows_left = (int)left;  // from the next step's first token on
     const int yrow = tid / (TO / 8), ycol = tid % (TO / 8) * 8;
     const int xrow = tid / (TH / 8), xcol = tid % (TH / 8) * 8;
     const uint32_t yat = ycol + 8 <= ywidth ? yrow * (uint32_t)yld + ycol * (int)sizeof(YT) : kNowhere;
@@ -395,7 +395,7 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
 #pragma unroll
         for (int b = 0; b < kFrags; ++b) read(f0, 0, 0, 0, b);
         int flip = 0;
-        for (int k = 0; k < left; k += 2 * kStepT) {
+        for (uint32_t k = 0; k < left; k += 2 * kStepT) {
             half(f0.x, f0.y, kFrags, [&](int b) { read(f1, flip, 0, 1, b); }, kPieces,
                  [&](int a) { store_piece(r[0], flip ^ kFlip, 0, a); });
             open_stage();
@@ -427,7 +427,7 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
         constexpr int kFirst = (kPieces + 2) / 3, kThen = 2 * kFirst < kPieces ? kFirst : kPieces - kFirst;
         constexpr int kLast = kPieces - kFirst - kThen;  // pieces of three sixths
         auto nothing = [](int) {};
-        for (int k = 0; k < left; k += kStepT) {
+        for (uint32_t k = 0; k < left; k += kStepT) {
             const int other = flip ^ kFlip;
             half(x0, y0, NI, [&](int b) { y1[b] = read_y(flip, 0, 0, 1, b); }, kFirst,
                  [&](int a) { store_piece(r, other, 0, a); });

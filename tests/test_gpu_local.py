@@ -150,6 +150,12 @@ GRAD = [
     (1, 4099, 64, 2500, 0, 0, F32, F32, False, None, 0, 0, "few"),
     (3, 129, 2056, 40, 1, 0, BF16, BF16, False, None, 0, 0, "none"),
     (1, 9000, 130, 1027, 2, 0, BF16, BF16, False, [8193], 0, 0, "any"),
+    # the last number of tokens that goes without sorting, and the next
+    (2, 256, 72, 33, 0, 0, F32, BF16, True, [256, 200], 0, 0, "few"),
+    (2, 257, 72, 33, 0, 0, BF16, BF16, False, [257, 64], 0, 0, "few"),
+    (3, 200, 24, 40000, 3, -7, BF16, F32, False, None, 0, 1, "one"),
+    (1, 300, 4100, 3, 0, 0, BF16, BF16, False, None, 1, 0, "any"),
+    (2, 400, 1, 70001, 0, 0, F32, F32, True, None, 0, 0, "any"),
 ]
 
 
@@ -486,6 +492,69 @@ def test_act_wgrad_repeats_bit_for_bit():
     for _ in range(3):
         run_wgrad(dy, q, s, b)
         assert torch.equal(a, b)
+
+
+# ---- far offsets ----
+
+
+def test_rows_past_2_31_elements():
+    # two replica and gradient rows of 1.2e9 bf16 elements, the table and the
+    # weight at their ends: element offsets beyond 2^31, bytes beyond 2^32
+    n, v, h, o, t = 2, 7, 40, 9, 300
+    ld, off = 1_200_000_000, 1_200_000_000 - 7 * 40 - 9 * 40
+    rows = torch.zeros((n, ld), dtype=BF16, device=DEV)
+    rows[:, off:] = torch.randn((n, ld - off), generator=gen(40), device=DEV).to(BF16)
+    small = rows[:, off:].clone()
+    tok = draw_ids("any", n, t, v, 0, True)
+    out, ref = torch.empty((2, n, t, h), dtype=BF16, device=DEV)
+    ll.ll_embed(tok, rows, out, v=v, offset=off)
+    ll.ll_embed(tok, small, ref, v=v)
+    assert torch.equal(out, ref) and out.abs().sum() > 0
+    q = torch.empty((n, t, h), dtype=torch.uint8, device=DEV)
+    s = torch.empty((n, t, 2), dtype=torch.uint8, device=DEV)
+    ll.ll_act_pack(out, q, s)
+    dy = torch.randn((n, t, o), generator=gen(41), device=DEV).to(BF16)
+    rows.zero_()
+    small.zero_()
+    for g, base in ((rows, off), (small, 0)):
+        run_embed_grad(tok, out, g, v=v, offset=base)
+        run_wgrad(dy, q, s, g, offset=base + v * h)
+    assert torch.equal(rows[:, off:], small) and small.abs().sum() > 0
+    assert not rows[:, :off].any()
+
+
+def test_activations_past_2_31_elements():
+    # token rows at the end of 2.2e9 elements; only the last tokens are filled
+    n, t, h = 1, 68000, 96
+    ld = 32768
+    x = torch.zeros((n, t, ld), dtype=BF16, device=DEV)[:, :, :h]
+    q = torch.zeros((n, t, ld), dtype=torch.uint8, device=DEV)[:, :, :h]
+    s = torch.zeros((n, t, 3), dtype=torch.uint8, device=DEV)
+    m = 500
+    x[:, -m:] = ints((n, m, h), -3, 3, 42, BF16)
+    ll.ll_act_pack(x, q, s)
+    back = torch.zeros((n, t, ld), dtype=BF16, device=DEV)[:, :, :h]
+    ll.ll_act_unpack(q, s, back)
+    assert torch.equal(back[:, -m:], x[:, -m:]) and not back[:, :-m].any()
+    o = 8
+    dy = ints((n, t, o), -5, 5, 43, BF16)
+    grads = row_buffer(n, o * h, 0, F32)
+    run_wgrad(dy, q, s, grads)
+    want = torch.mm(dy[0, -m:].double().t().contiguous(), x[0, -m:].double())
+    assert torch.equal(grads[0, : o * h].view(o, h).double(), want)
+    tok = torch.full((n, t), -1, dtype=torch.int32, device=DEV)
+    tok[0, -m:] = torch.randint(0, 4, (m,), generator=gen(44), device=DEV, dtype=torch.int32)
+    grads = row_buffer(n, 4 * h, 0, F32)
+    run_embed_grad(tok, x, grads, v=4)
+    want = torch.zeros((4, h), dtype=torch.float64, device=DEV)
+    want.index_add_(0, tok[0, -m:].long(), x[0, -m:].double())
+    assert torch.equal(grads[0, : 4 * h].view(4, h).double(), want)
+    big = torch.zeros((n, t, ld), dtype=BF16, device=DEV)[:, :, :h]
+    table = row_buffer(1, 4 * h, 0, BF16)
+    table.normal_(generator=gen(45))
+    ll.ll_embed(tok, table, big, v=4)
+    assert torch.equal(big[0, -m:], table[0, : 4 * h].view(4, h)[tok[0, -m:].long()])
+    assert not big[0, :-m].any()
 
 
 # ---- together ----------------------------------------------------------------------

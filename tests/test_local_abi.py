@@ -91,7 +91,14 @@ CASES += [("ll_act_wgrad", *c) for c in [
     (dict(ydtype=3), -1, "ydtype"), (dict(grads=None), -1, "grads is NULL"),
     (dict(offset=8), -1, "exceed"), (dict(dy=None), -1, "dy is NULL"),
     (dict(ld_y=2), -1, "dy: ld=2"), (dict(q=None), -1, "q is NULL"), (dict(s=None), -1, "s is NULL"),
-    (dict(ld_q=39), -1, "q: ld"), (dict(ld_g=124), -2, "multiple of 16")]]
+    (dict(ld_q=39), -1, "q: ld"), (dict(ld_g=124), -2, "multiple of 16"),
+    (dict(ld_y=1 << 24), -1, "2^24"), (dict(ld_q=1 << 24), -1, "2^24"),
+    (dict(ld_s=1 << 24), -1, "2^24")]]
+# more workgroups than a grid holds
+CASES += [("ll_embed_grad", dict(n=1024, t=300, h=1, v=1 << 24, ld_t=300, ld_y=1, ld_g=1 << 24), -1,
+           "too many workgroups"),
+          ("ll_act_wgrad", dict(n=1024, t=1, o=1 << 20, h=1 << 7, ld_y=1 << 20, ld_q=1 << 7, ld_s=4,
+                                ld_g=1 << 27), -1, "too many workgroups")]
 
 
 @pytest.mark.parametrize("func,change,code,frag", CASES)
