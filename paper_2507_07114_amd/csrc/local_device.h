@@ -30,14 +30,6 @@ __device__ __forceinline__ T narrow(float x) {
     return (T)x;  // round to nearest even
 }
 
-// Columns of one unit: 16 bytes of the narrowest of its types, so that a
-// wavefront's access to that type is 1 KiB of consecutive memory.
-template <class A, class B>
-constexpr int unit_of() {
-    return 16 / (int)(sizeof(typename A::T) < sizeof(typename B::T) ? sizeof(typename A::T)
-                                                                   : sizeof(typename B::T));
-}
-
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 

@@ -16,14 +16,15 @@ namespace {
 // and written past them.  8 workers' 8192 tokens of 4096 bf16 columns, us: this
 // 147 to 150; 64 lanes 155; 256 lanes 150; four units of a lane in flight 154;
 // rows dealt out flat, as in local_act.hip, 163; written through the caches 180.
-// The distinct rows and the output are 752 MB (5.0 TB/s of them), the rows
+// A unit is 16 bytes of the output, one store: 4 x 8192 x 4096 from bf16 to fp32
+// rows take 104, 216 with units of 16 bytes of the table.  The distinct rows and the output are 752 MB (5.0 TB/s of them), the rows
 // read with repetitions 1062 MB.
 
 template <class R, class O>
 __global__ __launch_bounds__(kBlock) void k_embed(EmbedParams p, int lanes) {
     typedef typename R::T RT;
     typedef typename O::T OT;
-    constexpr int U = unit_of<R, O>();
+    constexpr int U = 16 / (int)sizeof(OT);
     const int rows = kBlock / lanes, lane = threadIdx.x % lanes;
     const int64_t total = (int64_t)p.n * p.t;
     const int64_t units = (p.h + U - 1) / U;
@@ -284,7 +285,8 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradParams& p, const GradPl
                     for (int c = 0; c < U; ++c)
                         out[c] = p.accumulate ? __builtin_fmaf(p.scale, sum[c], out[c])
                                               : p.scale * sum[c];
-                    store_unit<GT, U, true>(d, have, out);
+                    // two accesses to a unit (bf16 dy, fp32 grads) meet in the cache
+                    store_unit<GT, U, U * sizeof(GT) <= 16>(d, have, out);
                 }
             }
 #pragma unroll
@@ -300,7 +302,7 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradParams& p, const GradPl
 template <class Y, class G>
 __device__ __forceinline__ void zero_rows(const EmbedGradParams& p, const GradPlan& g, int64_t b) {
     typedef typename G::T GT;
-    constexpr int U = unit_of<Y, G>(), kTurns = kRowUnits / kBlock;
+    constexpr int U = 16 / (int)sizeof(GT), kTurns = kRowUnits / kBlock;
     const int64_t span = b % g.rows.spans, group = b / g.rows.spans;
     const int i = (int)(group / g.rows.groups);
     const int64_t r0 = (group - i * g.rows.groups) * g.rows.rows;
@@ -393,12 +395,14 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, G
 
 // Few tokens: one launch, without sorting.  A workgroup takes table rows of about
 // 8 KiB (or a piece of a wide row), looks all the worker's tokens through, keeps
-// those of its rows in order, and each lane adds up its unit's.
+// those of its rows in order, and each lane adds up its unit's.  Accumulating, it
+// takes the row of one token, unless an earlier token names it (4 workers' 256
+// tokens of 32000 x 4096: ACCB us, ACCA by table rows).
 template <class Y, class G>
 __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, RowBlocks g) {
     typedef typename Y::T YT;
     typedef typename G::T GT;
-    constexpr int U = unit_of<Y, G>();
+    constexpr int U = 16 / (int)sizeof(GT);
     constexpr int kWaves = kBlock / kWave;
     constexpr int kAhead = 4;  // tokens whose loads are in flight
     __shared__ uint16_t place[kFewTokens];
@@ -406,9 +410,13 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
     __shared__ int found[kWaves];
     const int64_t span = blockIdx.x % g.spans, group = blockIdx.x / g.spans;
     const int i = (int)(group / g.groups);
-    const int64_t r0 = (group - i * g.groups) * g.rows;
-    const int rows = (int)(p.tok.v - r0 < g.rows ? p.tok.v - r0 : g.rows);
     const int m = (int)batch_len(p.lengths, i, p.t), j = threadIdx.x;
+    const int place0 = (int)(group - i * g.groups);  // accumulating, the token's
+    const int64_t r0 = !p.accumulate ? (group - i * g.groups) * g.rows
+                       : place0 < m  ? table_row(p.tok, i, place0)
+                                     : -1;
+    if (r0 < 0) return;
+    const int rows = (int)(p.tok.v - r0 < g.rows ? p.tok.v - r0 : g.rows);
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
 
     // the tokens of these rows, in order of their places
@@ -428,7 +436,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
         owner[at] = (uint8_t)row;
     }
     __syncthreads();
-    if (total == 0 && p.accumulate) return;
+    if (p.accumulate && place[0] < place0) return;
 
     const YT* dy = static_cast<const YT*>(p.dy.p) + (int64_t)i * p.t * p.dy.ld;
     GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + r0 * p.h;
@@ -462,7 +470,6 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
         }
         GT* d = grads + r * p.h + c0;
         if (p.accumulate) {
-            if (!any) continue;
             float old[U];
             load_unit<GT, U, false>(d, have, old);
 #pragma unroll
@@ -510,12 +517,12 @@ size_t grad_plan(int64_t n, int64_t t, int64_t h, int64_t v, uint8_t* ws, GradPl
 }
 
 // kRowUnits units to a workgroup, fewer rows where that leaves fewer workgroups
-// than two to a compute unit.
+// than two to a compute unit; one row where few tokens are accumulated.
 bool row_blocks(const EmbedGradParams& p, RowBlocks* g) {
-    const int64_t row = p.dy.bf16 || p.grads.bf16 ? (p.h + 7) / 8 : (p.h + 3) / 4;
+    const int64_t row = p.grads.bf16 ? (p.h + 7) / 8 : (p.h + 3) / 4;
     const int64_t fit = kRowUnits / row, few = p.n * p.tok.v / 512, rows = fit < few ? fit : few;
-    g->rows = (int)(rows < 1 ? 1 : (rows > kWave ? kWave : rows));
-    g->groups = (p.tok.v + g->rows - 1) / g->rows;
+    g->rows = p.accumulate ? 1 : (int)(rows < 1 ? 1 : (rows > kWave ? kWave : rows));
+    g->groups = p.accumulate ? p.t : (p.tok.v + g->rows - 1) / g->rows;
     g->spans = (g->rows * row + kRowUnits - 1) / kRowUnits;
     dim3 unused;
     return flat_rows(g->rows, row, 1, &g->units, &unused);
@@ -525,6 +532,7 @@ hipError_t launch_embed_grad_few(const EmbedGradParams& p, hipStream_t s) {
     RowBlocks g;
     if (!row_blocks(p, &g)) return hipErrorInvalidConfiguration;
     const int64_t blocks = p.n * g.groups * g.spans;
+    if (blocks == 0) return hipSuccess;
     if (blocks > 0xFFFFFFFFll / kBlock) return hipErrorInvalidConfiguration;
     LOSSY_LAUNCH2(k_embed_grad_few, p.dy.bf16, p.grads.bf16, dim3((unsigned)blocks), dim3(kBlock),
                   s, p, g);
@@ -535,7 +543,7 @@ hipError_t launch_embed_grad_few(const EmbedGradParams& p, hipStream_t s) {
 
 hipError_t launch_embed(const EmbedParams& p, hipStream_t s) {
     const int64_t rows = (int64_t)p.n * p.t;
-    const int u = p.table.bf16 || p.out.bf16 ? 8 : 4;
+    const int u = p.out.bf16 ? 8 : 4;
     const int lanes = lanes_per_row((p.h + u - 1) / u);
     const dim3 grid(grid_for((rows * lanes + kBlock - 1) / kBlock));
     LOSSY_LAUNCH2(k_embed, p.table.bf16, p.out.bf16, grid, dim3(kBlock), s, p, lanes);
