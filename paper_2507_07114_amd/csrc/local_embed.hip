@@ -14,11 +14,12 @@ namespace {
 // 128 lanes walk a row (fewer a short one, so that a workgroup takes more
 // rows).  Table rows are read through the caches, which hold the frequent ones,
 // and written past them.  8 workers' 8192 tokens of 4096 bf16 columns, us: this
-// 147 to 150; 64 lanes 155; 256 lanes 150; four units of a lane in flight 154;
+// 143 to 150; 64 lanes 155; 256 lanes 150; four units of a lane in flight 154;
 // rows dealt out flat, as in local_act.hip, 163; written through the caches 180.
+// The distinct rows and the output are 752 MB (5.3 TB/s of them); each die's L2
+// fetches rows for itself, 339 MB instead of 215.
 // A unit is 16 bytes of the output, one store: 4 x 8192 x 4096 from bf16 to fp32
-// rows take 104, 216 with units of 16 bytes of the table.  The distinct rows and the output are 752 MB (5.0 TB/s of them), the rows
-// read with repetitions 1062 MB.
+// rows take 103, with units of 16 bytes of the table 216.
 
 template <class R, class O>
 __global__ __launch_bounds__(kBlock) void k_embed(EmbedParams p, int lanes) {
@@ -66,6 +67,8 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedParams p, int lanes) {
 //    workgroups of the launch store zeros in the rows that have no token.
 // 3. k_embed_grad_join adds the partial sums of rows that cross chunks, in
 //    order.
+// Bound by HBM where the table is large: 8 workers' 8192 tokens, 25,695 x 4096
+// bf16, take 12 + 383 + 10 us, the main launch at 5.8 TB/s (mostly zeros).
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kMaxBins = 512;  // table rows a slice can hold: 32 KiB of counts
@@ -397,7 +400,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, G
 // 8 KiB (or a piece of a wide row), looks all the worker's tokens through, keeps
 // those of its rows in order, and each lane adds up its unit's.  Accumulating, it
 // takes the row of one token, unless an earlier token names it (4 workers' 256
-// tokens of 32000 x 4096: ACCB us, ACCA by table rows).
+// tokens of 32000 x 4096: 14 us with fp32 rows, 88 by table rows).
 template <class Y, class G>
 __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, RowBlocks g) {
     typedef typename Y::T YT;
