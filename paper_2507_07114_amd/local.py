@@ -42,6 +42,7 @@ _SIGNATURES.update({
 })
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice  # of a process that has GPU tensors
 
 _FLOATS = {torch.float32: LL_F32, torch.bfloat16: LL_BF16}
 _INTS = {torch.int32: LL_I32, torch.int64: LL_I64}
@@ -63,7 +64,7 @@ def _call(name: str, dev: int, *args) -> None:
     """The C entry point on the tensors' device and its current stream (the
     handle alone: a small call is bound by the host)."""
     fn = getattr(_load(), name)
-    if torch.cuda.current_device() == dev:
+    if _current_device() == dev:
         code = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
@@ -73,9 +74,10 @@ def _call(name: str, dev: int, *args) -> None:
 
 
 def _code(t: torch.Tensor, name: str, codes: dict) -> int:
-    if t.dtype not in codes:
+    code = codes.get(t.dtype)
+    if code is None:
         raise ValueError(f"{name} must be one of {[str(d) for d in codes]}, got {t.dtype}")
-    return codes[t.dtype]
+    return code
 
 
 def _act(t: torch.Tensor, name: str, n: int, tokens: int, width: Optional[int] = None) -> int:
@@ -97,29 +99,30 @@ def _act(t: torch.Tensor, name: str, n: int, tokens: int, width: Optional[int] =
 
 def _tokens(t: torch.Tensor) -> tuple:
     """(n, tokens, ld, integer code) of the token ids."""
-    if t.dim() != 2:
-        raise ValueError(f"tokens must be 2-D, got {tuple(t.shape)}")
-    n, m = t.shape
-    if m > 1 and t.stride(1) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2:
+        raise ValueError(f"tokens must be 2-D, got {tuple(shape)}")
+    n, m = shape
+    if stride[1] != 1 and m > 1:
         raise ValueError("tokens must have unit column stride")
-    return n, m, (t.stride(0) if n > 1 else max(m, 1)), _code(t, "tokens", _INTS)
+    return n, m, (stride[0] if n > 1 else max(m, 1)), _code(t, "tokens", _INTS)
 
 
-def _row_buffer(t: torch.Tensor, name: str, n: int) -> tuple:
-    """(ld, dtype code) of an [n][ld] row buffer."""
-    if t.dim() != 2 or t.shape[0] != n:
-        raise ValueError(f"{name} must be [{n}][ld], got {tuple(t.shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+def _row_buffer(t: torch.Tensor, name: str, n: int, offset: int, rows: int, h: int) -> tuple:
+    """(ld, dtype code) of an [n][ld] row buffer that holds rows x h elements
+    at `offset`."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != n:
+        raise ValueError(f"{name} must be [{n}][ld], got {tuple(shape)}")
+    width = shape[1]
+    if stride[1] != 1 and width > 1:
         raise ValueError(f"{name} must have unit column stride")
-    # one row: its stride counts where it is one, else its length
-    ld = t.stride(0) if n > 1 else max(t.stride(0), t.shape[1])
-    return ld, _code(t, name, _FLOATS)
-
-
-def _fits(t: torch.Tensor, name: str, offset: int, rows: int, h: int):
-    if offset < 0 or offset + rows * h > t.shape[1]:
+    if offset < 0 or offset + rows * h > width:
         raise ValueError(f"{name}: {rows} rows of {h} elements at offset {offset} exceed its "
-                         f"{t.shape[1]} columns")
+                         f"{width} columns")
+    # one row: its stride counts where it is one, else its length
+    ld = stride[0] if n > 1 else max(stride[0], width)
+    return ld, _code(t, name, _FLOATS)
 
 
 def _lens(t: Optional[torch.Tensor], n: int):
@@ -156,8 +159,7 @@ def ll_embed(tokens: torch.Tensor, replicas: torch.Tensor, out: torch.Tensor, *,
     n, m, ld_t, it = _tokens(tokens)
     ld_o = _act(out, "out", n, m)
     h = out.shape[2]
-    ld_r, rt = _row_buffer(replicas, "replicas", n)
-    _fits(replicas, "replicas", offset, v, h)
+    ld_r, rt = _row_buffer(replicas, "replicas", n, offset, v, h)
     ot, lens = _code(out, "out", _FLOATS), _lens(lengths, n)
     dev = _on_device("ll_embed", tokens, replicas, out, lengths)
     _call("ll_embed", dev, n, m, h, v, first, it, tokens.data_ptr(), ld_t, lens, rt,
@@ -177,8 +179,7 @@ def ll_embed_grad(tokens: torch.Tensor, dy: torch.Tensor, grads: torch.Tensor, *
     n, m, ld_t, it = _tokens(tokens)
     ld_y = _act(dy, "dy", n, m)
     h = dy.shape[2]
-    ld_g, gt = _row_buffer(grads, "grads", n)
-    _fits(grads, "grads", offset, v, h)
+    ld_g, gt = _row_buffer(grads, "grads", n, offset, v, h)
     yt, lens = _code(dy, "dy", _FLOATS), _lens(lengths, n)
     ws, ws_bytes = _ws(workspace)
     dev = _on_device("ll_embed_grad", tokens, dy, grads, lengths, workspace)
@@ -232,8 +233,7 @@ def ll_act_wgrad(dy: torch.Tensor, q: torch.Tensor, s: torch.Tensor, grads: torc
     h = q.shape[2]
     ld_y = _act(dy, "dy", n, m)
     ld_q, ld_s = _codes(q, s, n, m, h)
-    ld_g, gt = _row_buffer(grads, "grads", n)
-    _fits(grads, "grads", offset, o, h)
+    ld_g, gt = _row_buffer(grads, "grads", n, offset, o, h)
     yt, lens = _code(dy, "dy", _FLOATS), _lens(lengths, n)
     ws, ws_bytes = _ws(workspace)
     dev = _on_device("ll_act_wgrad", dy, q, s, grads, lengths, workspace)
