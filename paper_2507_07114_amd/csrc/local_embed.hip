@@ -226,10 +226,10 @@ __global__ __launch_bounds__(kSortThreads) void k_token_sort(int64_t t, const in
     }
 }
 
-// Up to so many tokens a worker the gradient takes one launch, without sorting.
-// us against the three launches: 8 workers' 256 tokens of 25,695 x 4096 bf16
-// 261 / 299, one worker's 256 of 32000 x 4096 45 / 56, 200 of 1000 x 2048 9 / 16, 256
-// of 50 x 512 (4 workers) 13 / 16; 500 of 60000 x 128 (2 workers) 60 / 23.
+// Up to so many tokens a worker the gradient takes one launch.  us against the
+// three launches: 8 workers' 256 tokens of 25,695 x 4096 bf16 250 / 299, one
+// worker's 256 of 32000 x 4096 44 / 56, 200 of 1000 x 2048 8 / 16, 256 of 50 x 512 (4
+// workers) 10 / 16.  Above, a row's tokens would follow each other for too long.
 constexpr int kFewTokens = kBlock;  // one to a thread
 
 // One wavefront of step 2.  U columns a lane; rows and places of the chunk lie
@@ -396,9 +396,9 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, G
     store_unit<GT, U, true>(d, have, out);
 }
 
-// Few tokens: one launch, without sorting.  A workgroup takes table rows of about
-// 8 KiB (or a piece of a wide row), looks all the worker's tokens through, keeps
-// those of its rows in order, and each lane adds up its unit's.  Accumulating, it
+// Few tokens: one launch.  A workgroup takes table rows of about 8 KiB (or a
+// piece of a wide row), looks all the worker's tokens through, groups the places
+// of those of its rows by row, in order, and each lane adds up its unit's.  Accumulating, it
 // takes the row of one token, unless an earlier token names it (4 workers' 256
 // tokens of 32000 x 4096: 14 us with fp32 rows, 88 by table rows).
 template <class Y, class G>
@@ -409,8 +409,9 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
     constexpr int kWaves = kBlock / kWave;
     constexpr int kAhead = 4;  // tokens whose loads are in flight
     __shared__ uint16_t place[kFewTokens];
-    __shared__ uint8_t owner[kFewTokens];
-    __shared__ int found[kWaves];
+    __shared__ int count[kWaves][kWave];  // a wavefront's tokens of each row
+    __shared__ int start[kWave + 1];      // a row's tokens are place[start ...]
+    __shared__ bool found[kWaves];
     const int64_t span = blockIdx.x % g.spans, group = blockIdx.x / g.spans;
     const int i = (int)(group / g.groups);
     const int m = (int)batch_len(p.lengths, i, p.t), j = threadIdx.x;
@@ -422,23 +423,49 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
     const int rows = (int)(p.tok.v - r0 < g.rows ? p.tok.v - r0 : g.rows);
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
 
-    // the tokens of these rows, in order of their places
-    const int64_t row = j < m ? table_row(p.tok, i, j) - r0 : -1;
-    const bool mine = row >= 0 && row < rows;
-    const uint64_t hits = __ballot(mine);
-    if (lane == 0) found[w] = __popcll(hits);
+    // the tokens of these rows, by row and place
+    const int64_t at_row = j < m ? table_row(p.tok, i, j) - r0 : -1;
+    const bool mine = at_row >= 0 && at_row < rows;
+    const int row = mine ? (int)at_row : 0;
+    uint64_t peers = __ballot(mine);
+    if (lane == 0) found[w] = peers != 0;
+    count[w][lane] = 0;
     __syncthreads();
-    int at = __popcll(hits & ((1ull << lane) - 1)), total = 0;
+    bool any = false;
 #pragma unroll
-    for (int a = 0; a < kWaves; ++a) {
-        at += a < w ? found[a] : 0;
-        total += found[a];
+    for (int a = 0; a < kWaves; ++a) any |= found[a];
+    if (any) {  // most workgroups of a large table have none
+        // the wavefront's tokens of the same row
+#pragma unroll
+        for (int b = 1; b < kWave; b *= 2) {
+            const uint64_t set = __ballot(row & b);
+            peers &= row & b ? set : ~set;
+        }
+        const int before = __popcll(peers & ((1ull << lane) - 1));
+        if (mine && before == 0) count[w][row] = __popcll(peers);
+        __syncthreads();
+        if (w == 0) {
+            int upto = 0;
+#pragma unroll
+            for (int a = 0; a < kWaves; ++a) upto += count[a][lane];
+#pragma unroll
+            for (int d = 1; d < kWave; d *= 2) {
+                const int x = __shfl_up(upto, d);
+                if (lane >= d) upto += x;
+            }
+            if (lane == 0) start[0] = 0;
+            start[lane + 1] = upto;
+        }
+        __syncthreads();
+        if (mine) {
+            int at = start[row] + before;
+#pragma unroll
+            for (int a = 0; a < kWaves; ++a)
+                if (a < w) at += count[a][row];
+            place[at] = (uint16_t)j;
+        }
+        __syncthreads();
     }
-    if (mine) {
-        place[at] = (uint16_t)j;
-        owner[at] = (uint8_t)row;
-    }
-    __syncthreads();
     if (p.accumulate && place[0] < place0) return;
 
     const YT* dy = static_cast<const YT*>(p.dy.p) + (int64_t)i * p.t * p.dy.ld;
@@ -450,26 +477,18 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
         const int r = (int)flat_row(g.units, u);
         const int64_t c0 = (int64_t)(u - r * g.units.units) * U, have = p.h - c0;
         float sum[U] = {};
-        bool any = false;
-        for (int k = 0; k < total;) {
-            int at[kAhead], n = 0;
-#pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
-                while (k < total && owner[k] != r) ++k;
-                at[a] = k < total ? place[k] : -1;
-                n += k < total;
-                ++k;
-            }
+        const int k0 = any ? start[r] : 0, k1 = any ? start[r + 1] : 0;
+        for (int k = k0; k < k1; k += kAhead) {
             float y[kAhead][U];
 #pragma unroll
             for (int a = 0; a < kAhead; ++a)
-                if (a < n) load_unit<YT, U, false>(dy + at[a] * p.dy.ld + c0, have, y[a]);
+                if (k + a < k1)
+                    load_unit<YT, U, false>(dy + place[k + a] * p.dy.ld + c0, have, y[a]);
 #pragma unroll
             for (int a = 0; a < kAhead; ++a)
-                if (a < n)
+                if (k + a < k1)
 #pragma unroll
                     for (int c = 0; c < U; ++c) sum[c] += y[a][c];
-            any |= n > 0;
         }
         GT* d = grads + r * p.h + c0;
         if (p.accumulate) {
@@ -480,7 +499,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
         } else {
             // an empty row is 0, not -0
 #pragma unroll
-            for (int c = 0; c < U; ++c) sum[c] = any ? p.scale * sum[c] : 0.0f;
+            for (int c = 0; c < U; ++c) sum[c] = k0 < k1 ? p.scale * sum[c] : 0.0f;
         }
         store_unit<GT, U, true>(d, have, sum);
     }
