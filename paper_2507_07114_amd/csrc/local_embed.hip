@@ -226,11 +226,15 @@ __global__ __launch_bounds__(kSortThreads) void k_token_sort(int64_t t, const in
     }
 }
 
-// Up to so many tokens a worker the gradient takes one launch.  us against the
-// three launches: 8 workers' 256 tokens of 25,695 x 4096 bf16 250 / 299, one
-// worker's 256 of 32000 x 4096 44 / 56, 200 of 1000 x 2048 8 / 16, 256 of 50 x 512 (4
-// workers) 10 / 16.  Above, a row's tokens would follow each other for too long.
-constexpr int kFewTokens = kBlock;  // one to a thread
+// Up to so many tokens a worker the gradient takes one launch, one token to a
+// thread: workgroups of 256 threads, or 512 where there are more tokens.  us
+// against the three launches: 8 workers' 256 tokens of 25,695 x 4096 bf16 250 /
+// 299 (263 by 512 threads), 4 workers' 256 of 50 x 512 10 / 16; 8 workers' 512 of
+// 25,695 x 4096 281 / 304, one worker's 512 of 32000 x 4096 48 / 56, 500 of 261 x
+// 184 9 / 15, 4 workers' 512 of 50 x 512 16.4 / 17.4.  1024 tokens by 1024 threads:
+// 4 workers' of 50 x 512 30 / 17, 8 workers' of 25,695 x 4096 324 / 312, one
+// worker's of 1867 x 1280 11 / 17.
+constexpr int kFewTokens = 512;
 
 // One wavefront of step 2.  U columns a lane; rows and places of the chunk lie
 // one to a lane.
@@ -396,19 +400,22 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, G
     store_unit<GT, U, true>(d, have, out);
 }
 
-// Few tokens: one launch.  A workgroup takes table rows of about 8 KiB (or a
-// piece of a wide row), looks all the worker's tokens through, groups the places
-// of those of its rows by row, in order, and each lane adds up its unit's.  Accumulating, it
-// takes the row of one token, unless an earlier token names it (4 workers' 256
-// tokens of 32000 x 4096: 14 us with fp32 rows, 88 by table rows).
-template <class Y, class G>
-__global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, RowBlocks g) {
+// Few tokens: one launch.  A workgroup of BLOCK threads takes table rows of 2
+// units a thread (or a piece of a wide row), looks all the worker's tokens
+// through, groups the places of those of its rows by row, in order, and each
+// lane adds up its unit's.  Accumulating, it takes the row of one token, unless
+// an earlier token names it (4 workers' 256 tokens of 32000 x 4096: 14 us with
+// fp32 rows, 88 by table rows).
+constexpr int kFewUnits = 2;
+
+template <class Y, class G, int BLOCK>
+__device__ __forceinline__ void few_rows(const EmbedGradParams& p, const RowBlocks& g) {
     typedef typename Y::T YT;
     typedef typename G::T GT;
     constexpr int U = 16 / (int)sizeof(GT);
-    constexpr int kWaves = kBlock / kWave;
+    constexpr int kWaves = BLOCK / kWave;
     constexpr int kAhead = 4;  // tokens whose loads are in flight
-    __shared__ uint16_t place[kFewTokens];
+    __shared__ uint16_t place[BLOCK];
     __shared__ int count[kWaves][kWave];  // a wavefront's tokens of each row
     __shared__ int start[kWave + 1];      // a row's tokens are place[start ...]
     __shared__ bool found[kWaves];
@@ -471,9 +478,9 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
     const YT* dy = static_cast<const YT*>(p.dy.p) + (int64_t)i * p.t * p.dy.ld;
     GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + r0 * p.h;
     const uint32_t all = rows * g.units.units;
-    const uint32_t u0 = (uint32_t)span * kRowUnits;
-    const uint32_t u1 = u0 + kRowUnits < all ? u0 + kRowUnits : all;
-    for (uint32_t u = u0 + threadIdx.x; u < u1; u += kBlock) {
+    const uint32_t u0 = (uint32_t)span * (BLOCK * kFewUnits);
+    const uint32_t u1 = u0 + BLOCK * kFewUnits < all ? u0 + BLOCK * kFewUnits : all;
+    for (uint32_t u = u0 + threadIdx.x; u < u1; u += BLOCK) {
         const int r = (int)flat_row(g.units, u);
         const int64_t c0 = (int64_t)(u - r * g.units.units) * U, have = p.h - c0;
         float sum[U] = {};
@@ -503,6 +510,16 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(EmbedGradParams p, Ro
         }
         store_unit<GT, U, true>(d, have, sum);
     }
+}
+
+template <class Y, class G>
+__global__ __launch_bounds__(256) void k_embed_grad_few_256(EmbedGradParams p, RowBlocks g) {
+    few_rows<Y, G, 256>(p, g);
+}
+
+template <class Y, class G>
+__global__ __launch_bounds__(512) void k_embed_grad_few_512(EmbedGradParams p, RowBlocks g) {
+    few_rows<Y, G, 512>(p, g);
 }
 
 size_t round16(size_t x) { return (x + 15) & ~(size_t)15; }
@@ -538,26 +555,31 @@ size_t grad_plan(int64_t n, int64_t t, int64_t h, int64_t v, uint8_t* ws, GradPl
     return at;
 }
 
-// kRowUnits units to a workgroup, fewer rows where that leaves fewer workgroups
+// `span` units to a workgroup, fewer rows where that leaves fewer workgroups
 // than two to a compute unit; one row where few tokens are accumulated.
-bool row_blocks(const EmbedGradParams& p, RowBlocks* g) {
+bool row_blocks(const EmbedGradParams& p, int64_t span, RowBlocks* g) {
     const int64_t row = p.grads.bf16 ? (p.h + 7) / 8 : (p.h + 3) / 4;
-    const int64_t fit = kRowUnits / row, few = p.n * p.tok.v / 512, rows = fit < few ? fit : few;
+    const int64_t fit = span / row, few = p.n * p.tok.v / 512, rows = fit < few ? fit : few;
     g->rows = p.accumulate ? 1 : (int)(rows < 1 ? 1 : (rows > kWave ? kWave : rows));
     g->groups = p.accumulate ? p.t : (p.tok.v + g->rows - 1) / g->rows;
-    g->spans = (g->rows * row + kRowUnits - 1) / kRowUnits;
+    g->spans = (g->rows * row + span - 1) / span;
     dim3 unused;
     return flat_rows(g->rows, row, 1, &g->units, &unused);
 }
 
 hipError_t launch_embed_grad_few(const EmbedGradParams& p, hipStream_t s) {
+    const int threads = p.t <= 256 ? 256 : 512;
     RowBlocks g;
-    if (!row_blocks(p, &g)) return hipErrorInvalidConfiguration;
+    if (!row_blocks(p, threads * kFewUnits, &g)) return hipErrorInvalidConfiguration;
     const int64_t blocks = p.n * g.groups * g.spans;
     if (blocks == 0) return hipSuccess;
-    if (blocks > 0xFFFFFFFFll / kBlock) return hipErrorInvalidConfiguration;
-    LOSSY_LAUNCH2(k_embed_grad_few, p.dy.bf16, p.grads.bf16, dim3((unsigned)blocks), dim3(kBlock),
-                  s, p, g);
+    if (blocks > 0xFFFFFFFFll / threads) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks);
+    if (threads == 256) {
+        LOSSY_LAUNCH2(k_embed_grad_few_256, p.dy.bf16, p.grads.bf16, grid, dim3(256), s, p, g);
+    } else {
+        LOSSY_LAUNCH2(k_embed_grad_few_512, p.dy.bf16, p.grads.bf16, grid, dim3(512), s, p, g);
+    }
     return hipGetLastError();
 }
 
@@ -587,7 +609,7 @@ hipError_t launch_embed_grad(const EmbedGradParams& p, void* ws, hipStream_t s) 
     g.chunk_blocks = (p.n * g.chunks * g.strips + 3) / 4;
     int64_t blocks = g.chunk_blocks;
     if (!p.accumulate) {
-        if (!row_blocks(p, &g.rows)) return hipErrorInvalidConfiguration;
+        if (!row_blocks(p, kRowUnits, &g.rows)) return hipErrorInvalidConfiguration;
         blocks += p.n * g.rows.groups * g.rows.spans;
     }
     const int64_t sorts = (int64_t)p.n << g.s.log_slices;

@@ -150,9 +150,13 @@ GRAD = [
     (1, 4099, 64, 2500, 0, 0, F32, F32, False, None, 0, 0, "few"),
     (3, 129, 2056, 40, 1, 0, BF16, BF16, False, None, 0, 0, "none"),
     (1, 9000, 130, 1027, 2, 0, BF16, BF16, False, [8193], 0, 0, "any"),
-    # the last number of tokens that goes without sorting, and the next
+    # 256, 512 and more tokens go different ways
     (2, 256, 72, 33, 0, 0, F32, BF16, True, [256, 200], 0, 0, "few"),
     (2, 257, 72, 33, 0, 0, BF16, BF16, False, [257, 64], 0, 0, "few"),
+    (3, 512, 24, 700, 1, 0, BF16, F32, False, None, 0, 0, "few"),
+    (2, 513, 24, 700, 0, 5, F32, BF16, True, [513, 500], 1, 0, "few"),
+    (1, 511, 5000, 9, 2, 0, F32, F32, False, None, 0, 1, "any"),
+    (2, 513, 9, 2, 0, 0, BF16, BF16, False, None, 0, 0, "one"),
     (3, 200, 24, 40000, 3, -7, BF16, F32, False, None, 0, 1, "one"),
     (1, 300, 4100, 3, 0, 0, BF16, BF16, False, None, 1, 0, "any"),
     (2, 400, 1, 70001, 0, 0, F32, F32, True, None, 0, 0, "any"),
