@@ -21,11 +21,6 @@ struct El16 {
 };
 
 template <class T>
-__device__ __forceinline__ float widen(T x) {
-    return (float)x;
-}
-
-template <class T>
 __device__ __forceinline__ T narrow(float x) {
     return (T)x;  // round to nearest even
 }
@@ -68,42 +63,99 @@ __device__ __forceinline__ void store_raw(void* p, typename RawOf<BYTES>::T v) {
     else *static_cast<V*>(p) = v;
 }
 
+// U consecutive elements as they lie in memory.  Loads that are to be in flight
+// together give these: a conversion inside a branch would wait for its load.
+template <class T, int U>
+struct Packed {
+    T e[U];
+};
+
+// U elements from p, all of which exist.
+template <class T, int U, bool STREAM>
+__device__ __forceinline__ Packed<T, U> load_packed(const T* p) {
+    constexpr int kStep = U * (int)sizeof(T) < 16 ? U : 16 / (int)sizeof(T);
+    Packed<T, U> r;
+#pragma unroll
+    for (int a = 0; a < U; a += kStep) {
+        auto v = load_raw<kStep*(int)sizeof(T), (int)sizeof(T), STREAM>(p + a);
+        __builtin_memcpy(r.e + a, &v, sizeof(v));
+    }
+    return r;
+}
+
+template <class T, int U>
+__device__ __forceinline__ void widen(const Packed<T, U>& r, float (&x)[U]) {
+#pragma unroll
+    for (int c = 0; c < U; ++c) x[c] = (float)r.e[c];
+}
+
+// U elements to p, rounded to T.
+template <class T, int U, bool STREAM>
+__device__ __forceinline__ void store_whole(T* p, const float (&x)[U]) {
+    constexpr int kStep = U * (int)sizeof(T) < 16 ? U : 16 / (int)sizeof(T);
+    T e[U];
+#pragma unroll
+    for (int c = 0; c < U; ++c) e[c] = narrow<T>(x[c]);
+#pragma unroll
+    for (int a = 0; a < U; a += kStep) {
+        typename RawOf<kStep*(int)sizeof(T)>::T v;
+        __builtin_memcpy(&v, e + a, sizeof(v));
+        store_raw<kStep*(int)sizeof(T), (int)sizeof(T), STREAM>(p + a, v);
+    }
+}
+
+// A lane's U columns of a row of h, those from c0 on being its own: it holds
+// columns at() .. at() + U, moved back to the row's last U where c0 + U passes
+// its end (then the first of them are another lane's, too).  A row shorter than U
+// is held from its first column.
+template <int U>
+struct Columns {
+    int64_t c0, h;
+    __device__ __forceinline__ int64_t at() const {
+        const int64_t last = h < U ? 0 : h - U;
+        return c0 < last ? c0 : last;
+    }
+    __device__ __forceinline__ bool whole() const { return h - c0 >= U; }
+    // the held columns of a row at p; NARROW: h < U, of which the last is repeated
+    template <class T, bool STREAM, bool NARROW>
+    __device__ __forceinline__ Packed<T, U> load(const T* p) const {
+        if (!NARROW) return load_packed<T, U, STREAM>(p + at());
+        Packed<T, U> r;
+#pragma unroll
+        for (int c = 0; c < U; ++c) r.e[c] = p[c < h ? c : h - 1];
+        return r;
+    }
+    // the lane's own of the held columns
+    template <class T, bool STREAM>
+    __device__ __forceinline__ void store(T* p, const float (&x)[U]) const {
+        if (whole()) {
+            store_whole<T, U, STREAM>(p + c0, x);
+        } else {
+            const int64_t c1 = at();
+#pragma unroll
+            for (int c = 0; c < U; ++c)
+                if (c1 + c >= c0 && c1 + c < h) p[c1 + c] = narrow<T>(x[c]);
+        }
+    }
+};
+
 // U consecutive elements from p, of which the first `have` exist (the others
 // read as 0).
 template <class T, int U, bool STREAM>
 __device__ __forceinline__ void load_unit(const T* p, int64_t have, float (&x)[U]) {
-    constexpr int kPer = 16 / (int)sizeof(T);  // elements of one access
-    constexpr int kStep = U < kPer ? U : kPer;
     if (have >= U) {
-        T e[U];
-#pragma unroll
-        for (int a = 0; a < U; a += kStep) {
-            auto v = load_raw<kStep*(int)sizeof(T), (int)sizeof(T), STREAM>(p + a);
-            __builtin_memcpy(e + a, &v, sizeof(v));
-        }
-#pragma unroll
-        for (int c = 0; c < U; ++c) x[c] = widen(e[c]);
+        widen(load_packed<T, U, STREAM>(p), x);
     } else {
 #pragma unroll
-        for (int c = 0; c < U; ++c) x[c] = c < have ? widen(p[c]) : 0.0f;
+        for (int c = 0; c < U; ++c) x[c] = c < have ? (float)p[c] : 0.0f;
     }
 }
 
 // The first `have` of U consecutive elements, rounded to T.
 template <class T, int U, bool STREAM>
 __device__ __forceinline__ void store_unit(T* p, int64_t have, const float (&x)[U]) {
-    constexpr int kPer = 16 / (int)sizeof(T);
-    constexpr int kStep = U < kPer ? U : kPer;
     if (have >= U) {
-        T e[U];
-#pragma unroll
-        for (int c = 0; c < U; ++c) e[c] = narrow<T>(x[c]);
-#pragma unroll
-        for (int a = 0; a < U; a += kStep) {
-            typename RawOf<kStep*(int)sizeof(T)>::T v;
-            __builtin_memcpy(&v, e + a, sizeof(v));
-            store_raw<kStep*(int)sizeof(T), (int)sizeof(T), STREAM>(p + a, v);
-        }
+        store_whole<T, U, STREAM>(p, x);
     } else {
 #pragma unroll
         for (int c = 0; c < U; ++c)
@@ -144,18 +196,21 @@ __device__ __forceinline__ int64_t table_row(const TokenView& tok, int i, int64_
     return table_row(tok, token_id(tok, i, j));
 }
 
-// Launch K<A, B> for the element types given as truth values (bf16?).
-#define LOSSY_LAUNCH2(K, a, b, grid, block, s, ...)                                         \
+// Launch K<A, B> for the element types given as truth values (bf16?), with `lds`
+// bytes of LDS besides the kernel's own.
+#define LOSSY_LAUNCH2_LDS(K, a, b, grid, block, lds, s, ...)                                \
     do {                                                                                    \
         if ((a) && (b))                                                                     \
-            hipLaunchKernelGGL((K<El16, El16>), grid, block, 0, s, __VA_ARGS__);            \
+            hipLaunchKernelGGL((K<El16, El16>), grid, block, lds, s, __VA_ARGS__);          \
         else if (a)                                                                         \
-            hipLaunchKernelGGL((K<El16, El32>), grid, block, 0, s, __VA_ARGS__);            \
+            hipLaunchKernelGGL((K<El16, El32>), grid, block, lds, s, __VA_ARGS__);          \
         else if (b)                                                                         \
-            hipLaunchKernelGGL((K<El32, El16>), grid, block, 0, s, __VA_ARGS__);            \
+            hipLaunchKernelGGL((K<El32, El16>), grid, block, lds, s, __VA_ARGS__);          \
         else                                                                                \
-            hipLaunchKernelGGL((K<El32, El32>), grid, block, 0, s, __VA_ARGS__);            \
+            hipLaunchKernelGGL((K<El32, El32>), grid, block, lds, s, __VA_ARGS__);          \
     } while (0)
+#define LOSSY_LAUNCH2(K, a, b, grid, block, s, ...) \
+    LOSSY_LAUNCH2_LDS(K, a, b, grid, block, 0, s, __VA_ARGS__)
 
 // A grid of at most 2^20 workgroups (kernels stride over the rest).
 inline unsigned grid_for(int64_t blocks) {

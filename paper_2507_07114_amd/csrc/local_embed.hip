@@ -21,8 +21,8 @@ namespace {
 // A unit is 16 bytes of the output, one store: 4 x 8192 x 4096 from bf16 to fp32
 // rows take 103, with units of 16 bytes of the table 216.
 
-template <class R, class O>
-__global__ __launch_bounds__(kBlock) void k_embed(EmbedParams p, int lanes) {
+template <class R, class O, bool NARROW>
+__device__ __forceinline__ void embed_rows(const EmbedParams& p, int lanes) {
     typedef typename R::T RT;
     typedef typename O::T OT;
     constexpr int U = 16 / (int)sizeof(OT);
@@ -40,16 +40,24 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedParams p, int lanes) {
         OT* dst = static_cast<OT*>(p.out.p) + tk * p.out.ld;
 #pragma unroll 1
         for (int64_t u = lane; u < units; u += lanes) {
-            const int64_t have = p.h - u * U;
+            const Columns<U> cols{u * U, p.h};
             float v[U] = {};
             if (row >= 0) {
-                load_unit<RT, U, false>(src + u * U, have, v);
+                widen(cols.template load<RT, false, NARROW>(src), v);
 #pragma unroll
                 for (int c = 0; c < U; ++c) v[c] *= p.scale;
             }
-            store_unit<OT, U, true>(dst + u * U, have, v);
+            // two lanes give the columns that both hold the same values
+            if (NARROW) cols.template store<OT, true>(dst, v);
+            else store_whole<OT, U, true>(dst + cols.at(), v);
         }
     }
+}
+
+template <class R, class O>
+__global__ __launch_bounds__(kBlock) void k_embed(EmbedParams p, int lanes) {
+    if (p.h < 16 / (int)sizeof(typename O::T)) embed_rows<R, O, true>(p, lanes);
+    else embed_rows<R, O, false>(p, lanes);
 }
 
 // ---- gradient ----------------------------------------------------------------
@@ -238,13 +246,13 @@ constexpr int kFewTokens = 512;
 
 // One wavefront of step 2.  U columns a lane; rows and places of the chunk lie
 // one to a lane.
-template <class Y, class G>
+template <class Y, class G, bool NARROW>
 __device__ __forceinline__ void sum_chunk(const EmbedGradParams& p, const GradPlan& g, int i,
                                           int64_t chunk, int64_t strip, int lane) {
     typedef typename Y::T YT;
     typedef typename G::T GT;
     constexpr int U = 16 / (int)sizeof(YT);
-    constexpr int kAhead = 4;  // tokens whose loads are in flight
+    constexpr int kAhead = 8;  // tokens whose loads are in flight
     // all of these loads at once; what lies behind the held tokens is not used
     const int32_t* rows = g.s.row + i * p.t;
     const int64_t k0 = chunk * g.chunk, k1 = k0 + g.chunk, last = p.t - 1;
@@ -257,44 +265,43 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradParams& p, const GradPl
     const int len = (int)(held - k0 < g.chunk ? held - k0 : g.chunk);
     before = k0 > 0 ? before : -1;
     after = k1 < held ? after : -1;
-    const int64_t c0 = (strip * kWave + lane) * U;
-    const int64_t have = p.h - c0;
-    const YT* dy = static_cast<const YT*>(p.dy.p) + i * p.t * p.dy.ld + c0;
-    GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + c0;
-    float* part = g.part + (i * g.chunks + chunk) * 2 * p.h + c0;
+    const Columns<U> cols{(strip * kWave + lane) * U, p.h};
+    const YT* dy = static_cast<const YT*>(p.dy.p) + i * p.t * p.dy.ld;
+    GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset;
+    float* part = g.part + (i * g.chunks + chunk) * 2 * p.h;
 
     float sum[U] = {};
     int cur = __builtin_amdgcn_readlane(my_row, 0);
     bool open = cur == before;  // the row began in an earlier chunk
     for (int k = 0; k < len; k += kAhead) {
-        float y[kAhead][U];
+        Packed<YT, U> y[kAhead];
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a)
-            if (k + a < len && have > 0)
-                load_unit<YT, U, true>(
-                    dy + (int64_t)__builtin_amdgcn_readlane(my_place, k + a) * p.dy.ld, have,
-                    y[a]);
+        for (int a = 0; a < kAhead; ++a) {  // past the end the last one again
+            const int at = k + a < len ? k + a : len - 1;
+            y[a] = cols.template load<YT, true, NARROW>(
+                dy + (int64_t)__builtin_amdgcn_readlane(my_place, at) * p.dy.ld);
+        }
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
             if (k + a >= len) break;
+            float x[U];
+            widen(y[a], x);
 #pragma unroll
-            for (int c = 0; c < U; ++c) sum[c] += y[a][c];
+            for (int c = 0; c < U; ++c) sum[c] += x[c];
             const int next = k + a + 1 < len ? __builtin_amdgcn_readlane(my_row, k + a + 1) : after;
             if (next == cur && k + a + 1 < len) continue;
-            if (have > 0) {
-                if (open || next == cur) {  // crosses into this chunk, or out of it
-                    store_unit<float, U, false>(part + (open ? 0 : p.h), have, sum);
-                } else {
-                    GT* d = grads + (int64_t)cur * p.h;
-                    float out[U];
-                    if (p.accumulate) load_unit<GT, U, false>(d, have, out);
+            if (open || next == cur) {  // crosses into this chunk, or out of it
+                cols.template store<float, false>(part + (open ? 0 : p.h), sum);
+            } else {
+                GT* d = grads + (int64_t)cur * p.h;
+                float out[U];
+                if (p.accumulate) widen(cols.template load<GT, false, NARROW>(d), out);
 #pragma unroll
-                    for (int c = 0; c < U; ++c)
-                        out[c] = p.accumulate ? __builtin_fmaf(p.scale, sum[c], out[c])
-                                              : p.scale * sum[c];
-                    // two accesses to a unit (bf16 dy, fp32 grads) meet in the cache
-                    store_unit<GT, U, U * sizeof(GT) <= 16>(d, have, out);
-                }
+                for (int c = 0; c < U; ++c)
+                    out[c] = p.accumulate ? __builtin_fmaf(p.scale, sum[c], out[c])
+                                          : p.scale * sum[c];
+                // two accesses to a unit (bf16 dy, fp32 grads) meet in the cache
+                cols.template store<GT, U * sizeof(GT) <= 16>(d, out);
             }
 #pragma unroll
             for (int c = 0; c < U; ++c) sum[c] = 0.0f;
@@ -320,22 +327,26 @@ __device__ __forceinline__ void zero_rows(const EmbedGradParams& p, const GradPl
 #pragma unroll
     for (int a = 0; a < kTurns; ++a) {
         const uint32_t u = u0 + a * kBlock;
-        count[a] = u < all ? g.s.count[g.s.at(i, r0 + flat_row(g.rows.units, u))] : 1;
+        count[a] = g.s.count[g.s.at(i, r0 + flat_row(g.rows.units, u < all ? u : all - 1))];
     }
     GT* grads = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + r0 * p.h;
     const float zero[U] = {};
 #pragma unroll
     for (int a = 0; a < kTurns; ++a) {
-        if (count[a]) continue;
         const uint32_t u = u0 + a * kBlock;
+        if (count[a] || u >= all) continue;
         const uint32_t r = flat_row(g.rows.units, u);
-        const int64_t c0 = (int64_t)(u - r * g.rows.units.units) * U;
-        store_unit<GT, U, true>(grads + r * p.h + c0, p.h - c0, zero);
+        const Columns<U> cols{(int64_t)(u - r * g.rows.units.units) * U, p.h};
+        if (p.h < U) cols.template store<GT, true>(grads + r * p.h, zero);
+        else store_whole<GT, U, true>(grads + r * p.h + cols.at(), zero);
     }
 }
 
+// 5 wavefronts to a SIMD, of 8 tokens in flight: 16 workers' 4096 tokens, 32000 x
+// 1024, bf16 into fp32, 352 us (6: 377, 4 of 8 tokens 372, 8 of 4 tokens 399);
+// the zeros go fastest with few writers.
 template <class Y, class G>
-__global__ __launch_bounds__(kBlock, 8) void k_embed_grad(EmbedGradParams p, GradPlan g) {
+__global__ __launch_bounds__(kBlock, 5) void k_embed_grad(EmbedGradParams p, GradPlan g) {
     if (blockIdx.x >= g.chunk_blocks) {
         zero_rows<Y, G>(p, g, blockIdx.x - g.chunk_blocks);
         return;
@@ -345,13 +356,16 @@ __global__ __launch_bounds__(kBlock, 8) void k_embed_grad(EmbedGradParams p, Gra
     if (w >= p.n * per) return;
     const int i = (int)(w / per);
     const int64_t c = (w - i * per) / g.strips;
-    sum_chunk<Y, G>(p, g, i, c, w - i * per - c * g.strips, threadIdx.x % kWave);
+    if (p.h < 16 / (int)sizeof(typename Y::T))
+        sum_chunk<Y, G, true>(p, g, i, c, w - i * per - c * g.strips, threadIdx.x % kWave);
+    else
+        sum_chunk<Y, G, false>(p, g, i, c, w - i * per - c * g.strips, threadIdx.x % kWave);
 }
 
 // Step 3: the wavefront of the chunk in which a crossing row begins adds the
 // row's partial sums up.
-template <class G>
-__global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, GradPlan g) {
+template <class G, bool NARROW>
+__device__ __forceinline__ void join_rows(const EmbedGradParams& p, const GradPlan& g) {
     typedef typename G::T GT;
     constexpr int U = 4;
     const int64_t strips = (p.h + kWave * U - 1) / (kWave * U);
@@ -361,8 +375,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, G
     const int i = (int)(w / per);
     const int64_t chunk = (w - i * per) / strips, strip = w - i * per - chunk * strips;
     const int lane = threadIdx.x % kWave;
-    const int64_t c0 = (strip * kWave + lane) * U;
-    const int64_t have = p.h - c0;
+    const Columns<U> cols{(strip * kWave + lane) * U, p.h};
     const int32_t* rows = g.s.row + i * p.t;
     const int64_t k0 = chunk * g.chunk, k1 = k0 + g.chunk, last = p.t - 1;
     const int held = g.s.held[i];
@@ -374,30 +387,36 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, G
     // the further chunks that hold the rest of its tokens
     const int here = __popcll(__ballot(lane < g.chunk && mine == row));
     const int more = (g.s.count[g.s.at(i, row)] - here + g.chunk - 1) / g.chunk;
-    const float* part = g.part + (i * g.chunks + chunk) * 2 * p.h + c0;
+    const float* part = g.part + (i * g.chunks + chunk) * 2 * p.h;
     float sum[U];
-    load_unit<float, U, false>(part + p.h, have, sum);
+    widen(cols.template load<float, false, NARROW>(part + p.h), sum);
     constexpr int kAhead = 8;  // partial sums whose loads are in flight
     for (int a0 = 1; a0 <= more; a0 += kAhead) {
-        float x[kAhead][U];
+        Packed<float, U> x[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {  // past the end the last one again
+            const int at = a0 + a <= more ? a0 + a : more;
+            x[a] = cols.template load<float, false, NARROW>(part + (int64_t)at * 2 * p.h);
+        }
 #pragma unroll
         for (int a = 0; a < kAhead; ++a)
             if (a0 + a <= more)
-                load_unit<float, U, false>(part + (int64_t)(a0 + a) * 2 * p.h, have, x[a]);
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a)
-            if (a0 + a <= more)
-#pragma unroll
-                for (int k = 0; k < U; ++k) sum[k] += x[a][k];
+                for (int k = 0; k < U; ++k) sum[k] += x[a].e[k];
     }
-    if (have <= 0) return;
-    GT* d = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + (int64_t)row * p.h + c0;
+    GT* d = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + (int64_t)row * p.h;
     float out[U];
-    if (p.accumulate) load_unit<GT, U, false>(d, have, out);
+    if (p.accumulate) widen(cols.template load<GT, false, NARROW>(d), out);
 #pragma unroll
     for (int a = 0; a < U; ++a)
         out[a] = p.accumulate ? __builtin_fmaf(p.scale, sum[a], out[a]) : p.scale * sum[a];
-    store_unit<GT, U, true>(d, have, out);
+    cols.template store<GT, true>(d, out);
+}
+
+template <class G>
+__global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, GradPlan g) {
+    if (p.h < 4) join_rows<G, true>(p, g);
+    else join_rows<G, false>(p, g);
 }
 
 // Few tokens: one launch.  A workgroup of BLOCK threads takes table rows of 2
@@ -408,7 +427,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_join(EmbedGradParams p, G
 // fp32 rows, 88 by table rows).
 constexpr int kFewUnits = 2;
 
-template <class Y, class G, int BLOCK>
+template <class Y, class G, int BLOCK, bool NARROW>
 __device__ __forceinline__ void few_rows(const EmbedGradParams& p, const RowBlocks& g) {
     typedef typename Y::T YT;
     typedef typename G::T GT;
@@ -480,27 +499,39 @@ __device__ __forceinline__ void few_rows(const EmbedGradParams& p, const RowBloc
     const uint32_t all = rows * g.units.units;
     const uint32_t u0 = (uint32_t)span * (BLOCK * kFewUnits);
     const uint32_t u1 = u0 + BLOCK * kFewUnits < all ? u0 + BLOCK * kFewUnits : all;
+    if (!any) {
+        const float zero[U] = {};
+        for (uint32_t u = u0 + threadIdx.x; u < u1; u += BLOCK) {
+            const uint32_t r = flat_row(g.units, u);
+            const Columns<U> cols{(int64_t)(u - r * g.units.units) * U, p.h};
+            if (NARROW) cols.template store<GT, true>(grads + r * p.h, zero);
+            else store_whole<GT, U, true>(grads + r * p.h + cols.at(), zero);
+        }
+        return;
+    }
     for (uint32_t u = u0 + threadIdx.x; u < u1; u += BLOCK) {
         const int r = (int)flat_row(g.units, u);
-        const int64_t c0 = (int64_t)(u - r * g.units.units) * U, have = p.h - c0;
+        const Columns<U> cols{(int64_t)(u - r * g.units.units) * U, p.h};
         float sum[U] = {};
-        const int k0 = any ? start[r] : 0, k1 = any ? start[r + 1] : 0;
+        const int k0 = start[r], k1 = start[r + 1];
         for (int k = k0; k < k1; k += kAhead) {
-            float y[kAhead][U];
+            Packed<YT, U> y[kAhead];
 #pragma unroll
-            for (int a = 0; a < kAhead; ++a)
-                if (k + a < k1)
-                    load_unit<YT, U, false>(dy + place[k + a] * p.dy.ld + c0, have, y[a]);
+            for (int a = 0; a < kAhead; ++a)  // past the end the last one again
+                y[a] = cols.template load<YT, false, NARROW>(
+                    dy + place[k + a < k1 ? k + a : k1 - 1] * p.dy.ld);
 #pragma unroll
-            for (int a = 0; a < kAhead; ++a)
-                if (k + a < k1)
+            for (int a = 0; a < kAhead; ++a) {
+                float x[U];
+                widen(y[a], x);
 #pragma unroll
-                    for (int c = 0; c < U; ++c) sum[c] += y[a][c];
+                for (int c = 0; c < U; ++c) sum[c] = k + a < k1 ? sum[c] + x[c] : sum[c];
+            }
         }
-        GT* d = grads + r * p.h + c0;
+        GT* d = grads + r * p.h;
         if (p.accumulate) {
             float old[U];
-            load_unit<GT, U, false>(d, have, old);
+            widen(cols.template load<GT, false, NARROW>(d), old);
 #pragma unroll
             for (int c = 0; c < U; ++c) sum[c] = __builtin_fmaf(p.scale, sum[c], old[c]);
         } else {
@@ -508,18 +539,20 @@ __device__ __forceinline__ void few_rows(const EmbedGradParams& p, const RowBloc
 #pragma unroll
             for (int c = 0; c < U; ++c) sum[c] = k0 < k1 ? p.scale * sum[c] : 0.0f;
         }
-        store_unit<GT, U, true>(d, have, sum);
+        cols.template store<GT, true>(d, sum);
     }
 }
 
 template <class Y, class G>
 __global__ __launch_bounds__(256) void k_embed_grad_few_256(EmbedGradParams p, RowBlocks g) {
-    few_rows<Y, G, 256>(p, g);
+    if (p.h < 16 / (int)sizeof(typename G::T)) few_rows<Y, G, 256, true>(p, g);
+    else few_rows<Y, G, 256, false>(p, g);
 }
 
 template <class Y, class G>
 __global__ __launch_bounds__(512) void k_embed_grad_few_512(EmbedGradParams p, RowBlocks g) {
-    few_rows<Y, G, 512>(p, g);
+    if (p.h < 16 / (int)sizeof(typename G::T)) few_rows<Y, G, 512, true>(p, g);
+    else few_rows<Y, G, 512, false>(p, g);
 }
 
 size_t round16(size_t x) { return (x + 15) & ~(size_t)15; }
@@ -576,7 +609,11 @@ hipError_t launch_embed_grad_few(const EmbedGradParams& p, hipStream_t s) {
     if (blocks > 0xFFFFFFFFll / threads) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks);
     if (threads == 256) {
-        LOSSY_LAUNCH2(k_embed_grad_few_256, p.dy.bf16, p.grads.bf16, grid, dim3(256), s, p, g);
+        // LDS that nothing uses: 6 workgroups to a compute unit.  4 workers' 256 tokens
+        // of 32000 x 4096, us: bf16 155, fp32 319; with 8 workgroups 173, 336; with 5
+        // 173, 340.
+        LOSSY_LAUNCH2_LDS(k_embed_grad_few_256, p.dy.bf16, p.grads.bf16, grid, dim3(256), 24000,
+                          s, p, g);
     } else {
         LOSSY_LAUNCH2(k_embed_grad_few_512, p.dy.bf16, p.grads.bf16, grid, dim3(512), s, p, g);
     }
