@@ -63,30 +63,40 @@ __device__ __forceinline__ void store_raw(void* p, typename RawOf<BYTES>::T v) {
     else *static_cast<V*>(p) = v;
 }
 
-// U consecutive elements as they lie in memory.  Loads that are to be in flight
-// together give these: a conversion inside a branch would wait for its load.
+// U consecutive elements as they lie in memory, in words: loads that are to be in
+// flight together give these.  A conversion inside a branch, elements that a
+// branch leaves apart too, would wait for their load.
 template <class T, int U>
 struct Packed {
-    T e[U];
+    uint32_t w[U * (int)sizeof(T) / 4];
 };
 
 // U elements from p, all of which exist.
 template <class T, int U, bool STREAM>
 __device__ __forceinline__ Packed<T, U> load_packed(const T* p) {
-    constexpr int kStep = U * (int)sizeof(T) < 16 ? U : 16 / (int)sizeof(T);
+    constexpr int kBytes = U * (int)sizeof(T), kStep = kBytes < 16 ? kBytes : 16;
     Packed<T, U> r;
 #pragma unroll
-    for (int a = 0; a < U; a += kStep) {
-        auto v = load_raw<kStep*(int)sizeof(T), (int)sizeof(T), STREAM>(p + a);
-        __builtin_memcpy(r.e + a, &v, sizeof(v));
+    for (int a = 0; a < kBytes; a += kStep) {
+        auto v = load_raw<kStep, (int)sizeof(T), STREAM>(reinterpret_cast<const uint8_t*>(p) + a);
+        __builtin_memcpy(r.w + a / 4, &v, sizeof(v));
     }
     return r;
 }
 
-template <class T, int U>
-__device__ __forceinline__ void widen(const Packed<T, U>& r, float (&x)[U]) {
+template <int U>
+__device__ __forceinline__ void widen(const Packed<float, U>& r, float (&x)[U]) {
 #pragma unroll
-    for (int c = 0; c < U; ++c) x[c] = (float)r.e[c];
+    for (int c = 0; c < U; ++c) x[c] = __uint_as_float(r.w[c]);
+}
+
+template <int U>
+__device__ __forceinline__ void widen(const Packed<__bf16, U>& r, float (&x)[U]) {
+#pragma unroll
+    for (int c = 0; c < U; c += 2) {
+        x[c] = __uint_as_float(r.w[c / 2] << 16);
+        x[c + 1] = __uint_as_float(r.w[c / 2] & 0xFFFF0000u);
+    }
 }
 
 // U elements to p, rounded to T.
@@ -120,9 +130,11 @@ struct Columns {
     template <class T, bool STREAM, bool NARROW>
     __device__ __forceinline__ Packed<T, U> load(const T* p) const {
         if (!NARROW) return load_packed<T, U, STREAM>(p + at());
-        Packed<T, U> r;
+        T e[U];
 #pragma unroll
-        for (int c = 0; c < U; ++c) r.e[c] = p[c < h ? c : h - 1];
+        for (int c = 0; c < U; ++c) e[c] = p[c < h ? c : h - 1];
+        Packed<T, U> r;
+        __builtin_memcpy(r.w, e, sizeof(r.w));
         return r;
     }
     // the lane's own of the held columns
@@ -168,13 +180,6 @@ __device__ __forceinline__ int64_t batch_len(const int32_t* lengths, int i, int6
     if (!lengths) return t;
     const int64_t m = lengths[i];
     return m < 0 ? 0 : (m > t ? t : m);
-}
-
-// Whether token row tk = i * t + j lies inside its worker's batch.
-__device__ __forceinline__ bool in_batch(const int32_t* lengths, uint32_t tk, int64_t t) {
-    if (!lengths) return true;
-    const uint32_t i = tk / (uint32_t)t;
-    return (int64_t)(tk - i * (uint32_t)t) < lengths[i];
 }
 
 // Table row of a token, or -1 where the table does not hold it.  Held ids are

@@ -402,7 +402,7 @@ __device__ __forceinline__ void join_rows(const EmbedGradParams& p, const GradPl
         for (int a = 0; a < kAhead; ++a)
             if (a0 + a <= more)
 #pragma unroll
-                for (int k = 0; k < U; ++k) sum[k] += x[a].e[k];
+                for (int k = 0; k < U; ++k) sum[k] += __uint_as_float(x[a].w[k]);
     }
     GT* d = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset + (int64_t)row * p.h;
     float out[U];
