@@ -471,6 +471,20 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kPadded;
 #pragma unroll
     for (int c = 0; c < NI; ++c) {
+        typedef typename G::T GT;
+        constexpr int U = 16 / (int)sizeof(GT), kLanes = kWide / U, kRows = kWave / kLanes;
+        const int64_t h = h0 + wh + lane % kLanes * U;
+        GT* d = static_cast<GT*>(p.grads.p) + i * p.grads.ld + p.grads.offset +
+                (o0 + wo + c * 32 + lane / kLanes) * p.h + h;
+        const int64_t rows = p.o - (o0 + wo + c * 32 + lane / kLanes);  // from d on
+        // what is added to, all loads at once
+        Packed<GT, U> old[32 / kRows] = {};
+        if (p.accumulate && !apart) {
+#pragma unroll
+            for (int r = 0; r < 32; r += kRows)
+                if (r < rows && p.h - h >= U)
+                    old[r / kRows] = load_packed<GT, U, false>(d + r * p.h);
+        }
 #pragma unroll
         for (int a = 0; a < MI; ++a)
 #pragma unroll
@@ -492,14 +506,22 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
                 store_unit<float, 4, false>(part + r * TH + lane % 16 * 4, 4, v);
             }
         } else {
-            constexpr int U = 16 / (int)sizeof(typename G::T), kLanes = kWide / U;
 #pragma unroll
-            for (int r = lane / kLanes; r < 32; r += kWave / kLanes) {
-                float v[U];
-                __builtin_memcpy(v, __builtin_assume_aligned(mine + r * kPadded + lane % kLanes * U, 16),
+            for (int r = 0; r < 32; r += kRows) {
+                float v[U], x[U];
+                __builtin_memcpy(v, __builtin_assume_aligned(mine + (r + lane / kLanes) * kPadded +
+                                                                 lane % kLanes * U, 16),
                                  sizeof(v));
-                const int64_t o = o0 + wo + c * 32 + r, h = h0 + wh + lane % kLanes * U;
-                if (o < p.o && h < p.h) put_sums<G, U>(p, i, o, h, v);
+                widen(old[r / kRows], x);
+                if (r >= rows || h >= p.h) continue;
+                if (p.h - h < U) {
+                    put_sums<G, U>(p, i, p.o - rows + r, h, v);
+                    continue;
+                }
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+                    v[k] = p.accumulate ? __builtin_fmaf(p.scale, v[k], x[k]) : p.scale * v[k];
+                store_whole<GT, U, true>(d + r * p.h, v);
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
