@@ -35,7 +35,8 @@ constexpr int kStepT = 32;    // tokens of a step
 // each, the other `rest` by `runs` workgroups over run_t tokens each, whose
 // fp32 sums (tile by tile, [rest][runs][edge][edge]) a second launch joins.
 struct WgradPlan {
-    int edge;  // of the square tiles
+    int edge;    // of the square tiles
+    bool light;  // light workgroups
     int64_t tiles_o, tiles_h, whole, rest;
     int runs;
     int64_t run_t;
@@ -190,9 +191,14 @@ constexpr int lds_bytes() {
     return 2 * 4 * kStepT * 2 * EDGE;
 }
 
+// LDS of a light workgroup: two steps of bf16 dy and codes take 32 KiB, the rows at
+// the end a little more.  Four such workgroups fit a compute unit.
+constexpr int kLightLds = 4 * 32 * 68 * 4;
+
 // A workgroup of WO x WH wavefronts owns a TO x TH tile of D over a run of
-// tokens.  TAILS: the tile's width or height is not a multiple of 8.
-template <class Y, class G, int TO, int TH, int WO, int WH, bool TAILS>
+// tokens.  TAILS: the tile's width or height is not a multiple of 8.  LIGHT: for few
+// tokens, where a tile is over before loads dealt out between products pay.
+template <class Y, class G, int TO, int TH, int WO, int WH, bool TAILS, bool LIGHT>
 __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan& g, Tile tile,
                                            int64_t ticket, int run, bool apart, uint8_t* lds) {
     typedef typename Y::T YT;
@@ -202,9 +208,11 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     constexpr int kRowY = TO * 2, kRowX = TH * 2;  // bytes of a tile row
     constexpr int kStageY = kStepT * kRowY, kStageX = kStepT * kRowX;
     constexpr int kAllY = kTerms * kStageY, kStage = kAllY + kStageX;
-    // half of the LDS, a power of two: two stages of bf16 dy, one of fp32 dy
-    constexpr int kFlip = kTerms == 1 ? 2 * kStage : kStage;
-    static_assert(TO == TH && 2 * kFlip == lds_bytes<TO>(), "LDS");
+    // half of the LDS, a power of two: two stages of bf16 dy (LIGHT: one), one of
+    // fp32 dy
+    constexpr int kFlip = kTerms == 1 && !LIGHT ? 2 * kStage : kStage;
+    constexpr int kLds = LIGHT ? kLightLds : lds_bytes<TO>();
+    static_assert(TO == TH && 2 * kFlip <= kLds, "LDS");
     typedef Staged<Y, TO, TH, kThreads> Stage;
     const int i = tile.i;
     const int64_t o0 = tile.o0, h0 = tile.h0;
@@ -375,7 +383,29 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    if constexpr (kTerms == 1) {
+    if constexpr (LIGHT) {
+        // A step's tile goes into one half of the LDS while the other may still be
+        // read; the workgroups beside this one fill the waits.
+        Stage r;
+        load_stage(r);
+        int flip = 0;
+        auto nothing = [](int) {};
+        for (uint32_t k = 0; k < left; k += kStepT) {
+            store_stage(r, flip, 0);
+            load_stage(r);
+            barrier();
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                bf16x8 x[MI], y[NI];
+#pragma unroll
+                for (int b = 0; b < MI; ++b) x[b] = read_x(flip, 0, part, b);
+#pragma unroll
+                for (int b = 0; b < NI; ++b) y[b] = read_y(flip, 0, part, 0, b);
+                half(x, y, 0, nothing, 0, nothing);
+            }
+            flip ^= kFlip;
+        }
+    } else if constexpr (kTerms == 1) {
         // Two steps s, s + 1 multiply the stages of one half of the LDS, store
         // tiles s + 2, s + 3 into the other and load tiles s + 4, s + 5 into the
         // registers this frees.  The workgroup meets once, before the last
@@ -465,8 +495,14 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
     // A lane holds 4 x 4 consecutive columns of one row of every 32 x 32 block.
     // Through LDS, a wavefront's own part of it, they become whole row pieces:
     // 32 rows at a time, padded by 16 bytes against bank conflicts.
+    // Rows on 64-byte boundaries are written past the caches; the pieces of others
+    // meet there with their neighbours' (2 x 270 tokens, 6279 x 5110 fp32: 121 us past
+    // the caches, 91 through them; 6279 x 5120: 69, 79).
+    const bool past = ((uintptr_t)(static_cast<typename G::T*>(p.grads.p) + i * p.grads.ld +
+                                   p.grads.offset) |
+                       (uintptr_t)(p.h * (int64_t)sizeof(typename G::T))) % 64 == 0;
     constexpr int kWide = MI * 32, kPadded = kWide + 4;
-    static_assert(kWide == 64 && WO * WH * 32 * kPadded * 4 <= 2 * kFlip, "LDS of the end");
+    static_assert(kWide == 64 && WO * WH * 32 * kPadded * 4 <= kLds, "LDS of the end");
     barrier();
     float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kPadded;
 #pragma unroll
@@ -521,7 +557,17 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
 #pragma unroll
                 for (int k = 0; k < U; ++k)
                     v[k] = p.accumulate ? __builtin_fmaf(p.scale, v[k], x[k]) : p.scale * v[k];
-                store_whole<GT, U, true>(d + r * p.h, v);
+                // unlike barriers, or the compiler makes one store of both, through
+                // the caches
+                if (past) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    store_whole<GT, U, true>(d + r * p.h, v);
+                    __builtin_amdgcn_sched_barrier(0);
+                } else {
+                    __builtin_amdgcn_sched_barrier(1);
+                    store_whole<GT, U, false>(d + r * p.h, v);
+                    __builtin_amdgcn_sched_barrier(1);
+                }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -531,7 +577,7 @@ __device__ __forceinline__ void wgrad_tile(const WgradParams& p, const WgradPlan
 // The tile of a workgroup.  TAILS: o or h is not a multiple of 8; the tiles that
 // end there take a slower loop (4097 x 4099 x 4096 tokens: 158 us, 200 where all
 // tiles are 128 x 128; 4096 x 4096 with no such tile 116), which the others need not.
-template <class Y, class G, int EDGE, int WO, int WH, bool TAILS>
+template <class Y, class G, int EDGE, int WO, int WH, bool TAILS, bool LIGHT = false>
 __device__ __forceinline__ void wgrad_block(const WgradParams& p, const WgradPlan& g, uint8_t* lds) {
     const bool apart = g.runs > 1 && blockIdx.x >= g.whole;
     const int64_t ticket = apart ? blockIdx.x - g.whole : blockIdx.x;
@@ -539,9 +585,9 @@ __device__ __forceinline__ void wgrad_block(const WgradParams& p, const WgradPla
     const Tile tile =
         tile_at<EDGE, EDGE>(g, apart ? g.whole + ticket / g.runs : spread(ticket, g.whole));
     if (TAILS && ((p.o % 8 && p.o - tile.o0 < EDGE) || (p.h % 8 && p.h - tile.h0 < EDGE)))
-        wgrad_tile<Y, G, EDGE, EDGE, WO, WH, true>(p, g, tile, ticket, run, apart, lds);
+        wgrad_tile<Y, G, EDGE, EDGE, WO, WH, true, LIGHT>(p, g, tile, ticket, run, apart, lds);
     else
-        wgrad_tile<Y, G, EDGE, EDGE, WO, WH, false>(p, g, tile, ticket, run, apart, lds);
+        wgrad_tile<Y, G, EDGE, EDGE, WO, WH, false, LIGHT>(p, g, tile, ticket, run, apart, lds);
 }
 
 template <class Y, class G>
@@ -560,6 +606,12 @@ template <class Y, class G>
 __global__ __launch_bounds__(256, 2) void k_act_wgrad_128(WgradParams p, WgradPlan g) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[lds_bytes<128>()];
     wgrad_block<Y, G, 128, 2, 2, true>(p, g, lds);
+}
+
+template <class G>
+__global__ __launch_bounds__(256, 4) void k_act_wgrad_light(WgradParams p, WgradPlan g) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kLightLds];
+    wgrad_block<El16, G, 128, 2, 2, true, true>(p, g, lds);
 }
 
 // Sum of the runs of the tiles that were summed apart, in order.
@@ -594,53 +646,64 @@ __global__ __launch_bounds__(kBlock) void k_act_wgrad_join(WgradParams p, WgradP
     else join_tile<G, 128>(p, g);
 }
 
-// Microseconds of a plan, from measurements on square layers of 256 to 4096 and 64
-// to 8192 tokens: a launch with its first loads and last stores, and a step of 32
-// tokens where few compute units work, where each has a tile and, of 128 x 128
-// tiles, where each has two.  Sums kept apart cost 3 and 0.27 a megabyte.  bf16,
-// 2048 x 2048 and 512 tokens: 128 x 128 tiles in one run (12.1; two runs 33.5, 256 x
-// 256 18.8); 8192 tokens: 256 x 256 in four (77.4; one run 156.4, 128 x 128 89.8).
-// fp32, 2048 tokens: 128 x 128 in two (62.3; one 63.4, 256 x 256 in four 63.4).
+// Microseconds of a plan, from measurements on layers of 256 to 6000 columns and 2 to
+// 8192 tokens: a launch with its first loads and last stores, a step of 32 tokens
+// where few compute units work, where each has a tile and where each has as many
+// as fit, and what a further round of tiles costs besides its steps.  Sums kept
+// apart cost 3 and 0.27 a megabyte.  bf16 dy and gradients (256 x 256 / 128 x 128 /
+// light): 32 tokens, 4096 x 4096 13.0 / 16.6 / 10.7; 256 tokens 17.2 / 21.8 / 18.5; 4
+// workers' 128 tokens 48.6 / 58.6 / 40.7, 512 tokens 88.3 / 106.9 / 88.7; 512 tokens, 2048
+// x 2048 18.8 / 12.1 / 12.9; 3 workers' 10 tokens, 3936 x 5312 40 / 48 / 27.  Runs: 512
+// tokens, 2048 x 2048 by 128 x 128 tiles one 12.1, two 33.5; 8192 tokens by 256 x 256 four
+// 77.4, one 156.4; fp32, 2048 tokens by 128 x 128 two 62.3, one 63.4.
 constexpr int64_t kCus = 256;
 
 struct TileCost {
-    double launch, few, one, two;
+    int edge, places;  // workgroups that fit a compute unit
+    bool light;
+    double launch, few, one, all, round;
 };
-constexpr TileCost kCost[2][2] = {  // [bf16][256 x 256]
-    {{7.0, 0.83, 0.83, 1.40}, {11.0, 1.69, 2.30, 0.0}},
-    {{6.7, 0.35, 0.40, 0.55}, {9.0, 0.57, 0.80, 0.0}},
+constexpr TileCost kCost[2][3] = {  // [bf16]
+    {{256, 1, false, 11.0, 1.69, 2.30, 2.30, 9.0}, {128, 2, false, 7.0, 0.83, 0.83, 1.40, 4.5}},
+    {{256, 1, false, 11.0, 0.57, 0.80, 0.80, 9.0},
+     {128, 2, false, 6.7, 0.35, 0.40, 0.55, 4.5},
+     {128, 4, true, 5.9, 0.40, 0.44, 1.11, 4.3}},
 };
 
-double tiles_us(const TileCost& c, int64_t places, int64_t blocks, int64_t steps) {
-    const int64_t full = blocks / places, rest = blocks - full * places;
-    const double round = places > kCus ? c.two : c.one;
+double tiles_us(const TileCost& c, int64_t blocks, int64_t steps) {
+    const int64_t places = c.places * kCus, full = blocks / places, rest = blocks - full * places;
     const double last = rest == 0      ? 0.0
                         : rest <= kCus ? c.few + (c.one - c.few) * rest / kCus
-                                       : c.two;
-    return steps * (full * round + last);
+                                       : c.one + (c.all - c.one) * (rest - kCus) / (places - kCus);
+    // light workgroups end one by one
+    const double rounds = c.light ? (double)blocks / places : full + (rest > 0) - 1;
+    return steps * (full * c.all + last) + c.round * rounds;
 }
 
 void wgrad_plan(int64_t n, int64_t t, int64_t o, int64_t h, bool bf16, WgradPlan* g) {
     const int64_t steps = (t + kStepT - 1) / kStepT;
     double best = 0.0;
-    for (int edge = 256; edge >= 128; edge /= 2) {
-        const TileCost& cost = kCost[bf16][edge == 256];
+    for (const TileCost& cost : kCost[bf16]) {
+        if (cost.edge == 0) break;
+        const int edge = cost.edge;
         const int64_t tiles_o = (o + edge - 1) / edge, tiles_h = (h + edge - 1) / edge;
         const int64_t tiles = n * tiles_o * tiles_h;
-        const int64_t places = edge == 256 ? kCus : 2 * kCus;
+        const int64_t places = cost.places * kCus;
         for (int64_t runs = 1; runs <= 64 && (runs == 1 || runs * 2 <= steps); ++runs) {
+            if (runs > 1 && cost.light) break;
             const int64_t whole = runs == 1 ? tiles : tiles / places * places;
             const int64_t rest = tiles - whole;
             if (runs > 1 && (rest == 0 || rest * runs > 4 * kCus)) break;
             int64_t each = (steps + runs - 1) / runs;
             if (each < 1) each = 1;
-            double us = cost.launch + tiles_us(cost, places, whole, steps);
+            double us = cost.launch + (whole > 0 ? tiles_us(cost, whole, steps) : 0.0);
             if (runs > 1)
-                us += tiles_us(cost, places, rest * runs, each) + 3.0 +
-                      0.27e-6 * rest * runs * edge * edge * 4;
+                us += tiles_us(cost, rest * runs, each) + 3.0 +
+                      0.27e-6 * rest * runs * edge * edge * 4 + (whole > 0 ? cost.round : 0.0);
             if (g->edge && us >= best) continue;
             best = us;
             g->edge = edge;
+            g->light = cost.light;
             g->tiles_o = tiles_o;
             g->tiles_h = tiles_h;
             g->whole = whole;
@@ -672,7 +735,12 @@ hipError_t launch_act_wgrad(const WgradParams& p, void* ws, hipStream_t s) {
     const int64_t blocks = g.whole + g.rest * g.runs;
     if (blocks > 0xFFFFFFFFll / 512) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks);
-    if (g.edge == 256 && (p.o % 8 || p.h % 8)) {
+    if (g.light) {
+        if (p.grads.bf16)
+            hipLaunchKernelGGL((k_act_wgrad_light<El16>), grid, dim3(256), 0, s, p, g);
+        else
+            hipLaunchKernelGGL((k_act_wgrad_light<El32>), grid, dim3(256), 0, s, p, g);
+    } else if (g.edge == 256 && (p.o % 8 || p.h % 8)) {
         LOSSY_LAUNCH2(k_act_wgrad_256_tails, p.dy.bf16, p.grads.bf16, grid, dim3(512), s, p, g);
     } else if (g.edge == 256) {
         LOSSY_LAUNCH2(k_act_wgrad_256, p.dy.bf16, p.grads.bf16, grid, dim3(512), s, p, g);
