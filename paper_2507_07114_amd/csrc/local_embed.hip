@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedParams p, int lanes) {
 // 3. k_embed_grad_join adds the partial sums of rows that cross chunks, in
 //    order.
 // Bound by HBM where the table is large: 8 workers' 8192 tokens, 25,695 x 4096
-// bf16, take 12 + 383 + 10 us, the main launch at 5.8 TB/s (mostly zeros).
+// bf16, take 12 + 370 to 396 + 10 us, the main launch at 6 TB/s (mostly zeros).
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kMaxBins = 512;  // table rows a slice can hold: 32 KiB of counts
@@ -100,8 +100,8 @@ struct Sorted {
 };
 
 // Table rows dealt out to workgroups: kRowUnits units, of a few whole rows or a
-// piece of a wide one.  Zeros alone, 8 workers' 25,695 rows of 4096 bf16 columns,
-// us: 512 units 274 (6.1 TB/s), 256 323, 1024 313.
+// piece of a wide one.  16 workers' 4096 tokens, 32000 x 1024 fp32 rows, us: 512
+// units 352 (6.3 TB/s), 256 510, 1024 416.
 constexpr uint32_t kRowUnits = 512;
 
 struct RowBlocks {
