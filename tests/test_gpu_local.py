@@ -440,6 +440,8 @@ def test_act_wgrad(n, t, o, h, ydt, gdt, offset, lens, py, pq, ps, shift, accumu
                                      (3, 130, 770, 1030), (1, 700, 1025, 2049),
                                      (70, 37, 264, 520), (1, 290, 4096, 4104),
                                      (256, 100, 40, 16),
+                                     # few tokens, more tiles than fit at once
+                                     (3, 10, 2900, 3300), (1, 65, 4097, 4200),
                                      # a round of whole tiles and one cut into
                                      # runs; runs of large tiles; many runs
                                      (1, 1024, 4096, 4352), (1, 8192, 2048, 2040),
