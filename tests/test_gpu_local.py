@@ -244,6 +244,34 @@ def test_embed_grad_without_tokens_writes_zeros():
     assert (grads == SENTINEL).all()
 
 
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("t", [70, 400, 1500])
+def test_tokens_and_rows_inside_wider_ones(t, wide):
+    # ids in a slice of a wider tensor, tables in the middle of wider row buffers,
+    # workers of a batch cut from a larger one
+    n, h, v, off = 3, 37, 90, 11
+    tok = draw_ids("any", n, t, v, -3, wide)
+    wider = torch.full((n + 2, t + 13), -77, dtype=tok.dtype, device=DEV)
+    wider[1:-1, 5:5 + t] = tok
+    cut = wider[1:-1, 5:5 + t]
+    table = torch.randn((n, v * h), generator=gen(50), device=DEV).to(BF16)
+    rows = torch.full((n + 1, 8 * 1000), SENTINEL, dtype=BF16, device=DEV)
+    rows[1:, off:off + v * h] = table
+    plain = row_buffer(n, v * h, 0, BF16)
+    plain[:, :v * h] = table
+    out, ref = torch.empty((2, n, t, h), dtype=F32, device=DEV)
+    ll.ll_embed(cut, rows[1:, :4000], out, v=v, first=-3, offset=off)
+    ll.ll_embed(tok, plain, ref, v=v, first=-3)
+    assert torch.equal(out, ref) and out.abs().sum() > 0
+    dy = torch.randn((n, t, h), generator=gen(51), device=DEV)
+    before = rows.clone()
+    run_embed_grad(cut, dy, rows[1:, :4000], v=v, first=-3, offset=off)
+    run_embed_grad(tok, dy, plain, v=v, first=-3)
+    assert torch.equal(rows[1:, off:off + v * h], plain[:, :v * h])
+    rows[1:, off:off + v * h] = before[1:, off:off + v * h]
+    assert torch.equal(rows, before)
+
+
 def test_embed_grad_repeats_bit_for_bit():
     n, t, h, v = 2, 6000, 264, 500
     tok = draw_ids("few", n, t, v, 0, False)
