@@ -41,8 +41,10 @@ _SIGNATURES.update({
     "ll_act_wgrad_workspace_bytes": (_sz, [_i32, _i64, _i64, _i64]),
 })
 
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_current_device = torch._C._cuda_getDevice  # of a process that has GPU tensors
+# Called with GPU tensors in hand only; a torch without GPU support, where the
+# package can be imported all the same, has neither.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
 
 _FLOATS = {torch.float32: LL_F32, torch.bfloat16: LL_BF16}
 _INTS = {torch.int32: LL_I32, torch.int64: LL_I64}
