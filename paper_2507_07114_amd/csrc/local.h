@@ -1,5 +1,6 @@
 // Internal interface between the C ABI of the local-gradient operators
-// (local_api.cpp) and their HIP kernels (local.hip).
+// (local_api.cpp) and their HIP kernels (local_embed.hip, local_act.hip,
+// local_wgrad.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
