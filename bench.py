@@ -14,11 +14,11 @@ Throughput is algorithmic HBM bytes per second: arrived gradient packets
 read, master + moments read and written, arrived replica packets written
 and, for drift, stale replica packets read (lost gradient packets are never
 needed, so never counted).  Prints one JSON line on stdout.  Workloads
-smaller than 1 GiB get a 1 GiB scratch read between timed steps so that
+smaller than 1 GiB get a 1 GiB scratch read before every timed step so that
 they are not served from the 256 MB memory-side cache; their throughput is
 then taken over the per-step events.  Where a workload's workers take their
 gradients on their own replicas (n8_layer16m_bf16_adam), these are taken before
-every step and timed apart (local_gradients_ms).
+that read and timed apart (local_gradients_ms).
 """
 from __future__ import annotations
 
@@ -376,8 +376,8 @@ def main():
     footprint = sum(t.numel() * t.element_size()
                     for t in (dev.grads, dev.replicas, dev.theta, dev.m, dev.v) if t is not None)
     # A workload whose workers take their gradients on their replicas has them
-    # taken before every step, outside the step's events, and timed apart.
-    mall_flush = footprint < (1 << 30) and not w.layer
+    # taken before that, outside the step's events too, and timed apart.
+    mall_flush = footprint < (1 << 30)
     scratch = torch.zeros(1 << 28, dtype=torch.float32, device="cuda") if mall_flush else None
     if mall_flush and args.mall_flush == "read":
         from paper_2507_07114_amd import probe
