@@ -220,3 +220,22 @@ def test_many_workers(n, t, h, v, accumulate):
     x = torch.where(inside.unsqueeze(-1), ref, torch.zeros_like(ref))
     want = torch.bmm(dw.double().transpose(1, 2).contiguous(), x.double())
     assert torch.equal(wgrad[:, :o * h].view(n, o, h).double(), want)
+
+
+@pytest.mark.parametrize("t,o,h", [(40, 16, 64), (600, 4096, 4096)])
+@pytest.mark.parametrize("ydt", [BF16, F32])
+def test_act_wgrad_of_subnormal_dy(ydt, t, o, h):
+    # bf16 keeps 2^-133, and so do the matrix units
+    values = [2.0 ** -126, 2.0 ** -127, -(2.0 ** -130), 3 * 2.0 ** -133, 2.0 ** -133]
+    if ydt == F32:  # whose terms reach below 2^-126
+        values += [(1 + 2.0 ** -23) * 2.0 ** -110, (1 + 2.0 ** -15) * 2.0 ** -118]
+    dy = torch.zeros((1, t, o), dtype=ydt, device=DEV)
+    dy[0, t // 2, :len(values)] = torch.tensor(values, dtype=torch.float64).to(ydt).to(DEV)
+    assert dy[0, t // 2, :len(values)].double().tolist() == values
+    q = torch.full((1, t, h), 0x38, dtype=torch.uint8, device=DEV)  # 1.0
+    for k in (0, 40):
+        s = torch.full((1, t, (h + 31) // 32), 127 + k, dtype=torch.uint8, device=DEV)
+        grads = row_buffer(1, o * h, 0, F32)
+        run_wgrad(dy, q, s, grads)
+        want = dy[0, t // 2].double() * 2.0 ** k
+        assert torch.equal(grads[0, :o * h].view(o, h).double(), want[:, None].expand(o, h))
