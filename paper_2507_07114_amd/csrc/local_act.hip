@@ -1,6 +1,7 @@
 // 8-bit activation checkpoints (include/lossy_local.h): ll_act_pack and
 // ll_act_unpack.  Bound by HBM: 8 x 4096 x 11008 bf16 columns move 1093 MB each
-// way, at 6.1 TB/s over the two.
+// way, at 6.1 TB/s over the two in a long run of calls (5.1 in some of the first
+// twenty after a pause).
 #include <hip/hip_runtime.h>
 
 #include "local.h"

@@ -14,8 +14,9 @@ namespace {
 // 128 lanes walk a row (fewer a short one, so that a workgroup takes more
 // rows).  Table rows are read through the caches, which hold the frequent ones,
 // and written past them.  8 workers' 8192 tokens of 4096 bf16 columns, us: this
-// 143 to 150; 64 lanes 155; 256 lanes 150; four units of a lane in flight 154;
-// rows dealt out flat, as in local_act.hip, 163; written through the caches 180.
+// 144 a call among others (147 when the following were timed, 153 under a trace); 64
+// lanes 155; 256 lanes 150; four units of a lane in flight 154; rows dealt out
+// flat, as in local_act.hip, 163; written through the caches 180.
 // The distinct rows and the output are 752 MB (5.3 TB/s of them); each die's L2
 // fetches rows for itself, 339 MB instead of 215.
 // A unit is 16 bytes of the output, one store: 4 x 8192 x 4096 from bf16 to fp32
@@ -76,7 +77,8 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedParams p, int lanes) {
 // 3. k_embed_grad_join adds the partial sums of rows that cross chunks, in
 //    order.
 // Bound by HBM where the table is large: 8 workers' 8192 tokens, 25,695 x 4096
-// bf16, take 12 + 370 to 396 + 10 us, the main launch at 6 TB/s (mostly zeros).
+// bf16, take 12 + 369 to 416 + 10 us, the main launch at 5.4 to 6.0 TB/s (mostly
+// zeros; 394 a call in a long run of them).
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kMaxBins = 512;  // table rows a slice can hold: 32 KiB of counts

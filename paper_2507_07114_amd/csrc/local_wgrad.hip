@@ -8,10 +8,11 @@
 // tokens side by side: LDS holds the tiles as they come and the transposing
 // LDS read turns them.
 //
-// 4096 tokens, 4096 x 4096, bf16: 108 to 114 us, 1207 TFLOP/s and more (152 us with
-// 4 wavefronts a tile, 137 with 8 that meet twice a step, 125 once in two steps, 114
+// 4096 tokens, 4096 x 4096, bf16: 113 to 117 us, 1175 to 1216 TFLOP/s (152 us with 4
+// wavefronts a tile, 137 with 8 that meet twice a step, 125 once in two steps, 114
 // with reads, stores and loads dealt out between the products and rows stored
-// whole).  2 x 8192 tokens, 11008 x 4096: 1170 to 1240 us, 1190 TFLOP/s and more; the
+// whole).  2 x 8192 tokens, 11008 x 4096, in a long run of calls: 1200 to 1250 us,
+// 1181 to 1230 TFLOP/s; up to 1670 us in the first ten calls after a pause.  The
 // matrix units are busy in 65% of the cycles and LDS in 42%, at a clock that this
 // load holds at 1.6 to 1.8 GHz.
 #include <hip/hip_runtime.h>

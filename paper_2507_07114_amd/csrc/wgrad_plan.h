@@ -30,7 +30,9 @@ struct WgradPlan {
 // workers' 128 tokens 48.6 / 58.6 / 40.7, 512 tokens 88.3 / 106.9 / 88.7; 512 tokens, 2048
 // x 2048 18.8 / 12.1 / 12.9; 3 workers' 10 tokens, 3936 x 5312 40 / 48 / 27.  Runs: 512
 // tokens, 2048 x 2048 by 128 x 128 tiles one 12.1, two 33.5; 8192 tokens by 256 x 256 four
-// 77.4, one 156.4; fp32, 2048 tokens by 128 x 128 two 62.3, one 63.4.
+// 77.4, one 156.4; fp32, 2048 tokens by 128 x 128 two 62.3, one 63.4.  16384 tokens of
+// 512 x 1024 (32 tiles of 128 x 128) into fp32, events between the calls: 4 runs 49, 8
+// 36, 12 40, 16 39, 20 44, 24 45, 32 48; the model takes 16.
 constexpr int64_t kCus = 256;
 
 struct TileCost {
